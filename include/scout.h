@@ -385,6 +385,153 @@ int scout_layer_step(const scout_problem* p, const void* q, const void* digest,
                      void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * ---- Sequences that share a prefix.
+ *
+ * Several answers to one prompt, requests behind one system prompt, the beams of a
+ * search: their sequences begin with the same tokens, whose K and V tiles the pool
+ * holds once.  Two groups of entry points serve them:
+ *   pages    who holds which slot: a sequence is forked from another one without
+ *            its tiles being copied, freed, given slots for the blocks that it opens;
+ *            the pool is compacted
+ *   prefix   decode attention over the shared tokens, read once for all sequences
+ *
+ * Pages.  A slot may be named by the block tables of several sequences.  How many
+ * entries name it is kept in the pages' state, a buffer of scout_pages_bytes(n_slots)
+ * bytes in DEVICE memory, 16-byte aligned, whose first n_slots words are these counts
+ * (int32, 0: the slot is free) and whose rest is the library's.  scout_pages_init
+ * makes it from the block tables; from then on the calls below keep it current, and a
+ * table entry that they do not know of (one that the caller writes by itself) is a
+ * slot that they may give away.  Slots are taken lowest first, in the order of the
+ * takers, so that the same state gives the same slots.
+ *   - A row of the batch without a sequence has ctx_len -1: append_token leaves it
+ *     as it is, and it has no blocks.
+ *   - A shared tile is not written to: only full blocks are shared by a fork.
+ *     periodic_recall gives an evicted block's slot to another block of its pair, so
+ *     it is for pairs that hold their slots alone (fork with deep = 1).
+ *   - Calls on the same state must be ordered (one stream, or events).
+ *
+ * shared_prefix_attn reads nothing of the pages' state: prefix_table is a table of
+ * slots like any other.
+ */
+
+/* Bytes of the pages' state of a pool of n_slots slots (at most 2^29). */
+int scout_pages_bytes(int64_t n_slots, size_t* bytes);
+
+/*
+ * The pages' state of a cache that is there already: counts the entries of
+ * block_table that name a slot in [0, n_slots), of the first nb_b blocks of every
+ * sequence.
+ *   ctx_len      i32 [B]
+ *   block_table  i32 [B][Hkv][max_blocks]
+ *   pages        out
+ */
+int scout_pages_init(const scout_problem* p, const int32_t* ctx_len, const int32_t* block_table,
+                     int64_t n_slots, void* pages, size_t pages_bytes, void* stream);
+
+/*
+ * Slots for the blocks that the next append_token opens: for every sequence with
+ * t = ctx_len[b] >= 0, t % S == 0 and t < max_blocks * S, each KV head takes the
+ * lowest free slot, in the order of the pairs.  The others, and takers for whom none
+ * is left (then the caller keeps the block on the host, as append_token has it), get -1.
+ * A reserved slot counts as held from here on; the append that follows puts it into
+ * the table.
+ *   new_slot  i32 [B][Hkv]  out: append_token's argument
+ *   n_short   i32 [1]       out: takers for whom no slot was left
+ */
+int reserve_blocks(const scout_problem* p, const int32_t* ctx_len, int64_t n_slots, void* pages,
+                   size_t pages_bytes, int32_t* new_slot, int32_t* n_short, void* stream);
+
+/*
+ * Fork: sequence dst[i] becomes what src[i] is, with the same ctx_len, digests and
+ * blocks.
+ *   deep = 0  The child's table names the parent's slots (one more reference each),
+ *             except that of a last block that is not full: tokens will be added to
+ *             it, so its tiles are copied into a slot of the child's own.
+ *   deep = 1  Every block with a slot is copied into a slot of the child's own.
+ * Slots are the lowest free ones, in the order of the forks, KV heads and blocks; a
+ * block for which none is left is -1 in the child's table (its tiles are the
+ * caller's to hold on the host, as those of the blocks that are -1 in the parent's;
+ * host copies are the caller's to make).
+ * A fork is refused, and changes nothing, if src[i] or dst[i] is outside [0, B),
+ * dst[i] holds tokens (ctx_len > 0: free it first), is src of any fork of the call or
+ * dst of an earlier one.
+ *   src, dst  i32 [n], n <= B  DEVICE
+ *   digest, block_table, k_pool, v_pool, ctx_len   in/out, as in append_token
+ *   status    i32 [n]  out: -1 refused; else the number of blocks for which no slot was left
+ * Digests of blocks beyond the parent's last one are left as they were.
+ */
+int fork_sequences(const scout_problem* p, int32_t n, const int32_t* src, const int32_t* dst,
+                   int32_t deep, int32_t* ctx_len, void* digest, int32_t* block_table, void* k_pool,
+                   void* v_pool, int64_t n_slots, void* pages, size_t pages_bytes, int32_t* status,
+                   void* stream);
+
+/*
+ * Free: the listed sequences give back their references, a slot without references
+ * is free again, their table rows become -1 and their ctx_len -1.  Indices outside
+ * [0, B) are skipped, a sequence that is listed twice is freed once.
+ *   seq  i32 [n], n <= B  DEVICE
+ */
+int free_sequences(const scout_problem* p, int32_t n, const int32_t* seq, int32_t* ctx_len,
+                   int32_t* block_table, int64_t n_slots, void* pages, size_t pages_bytes, void* stream);
+
+/*
+ * Compaction: the n_live slots that are held become [0, n_live).  Those at n_live
+ * and beyond move, in ascending order, into the free ones below, in ascending order:
+ * tiles, counts, and every entry of block_table that names them (all max_blocks of a
+ * row).  Slots that are named elsewhere (a prefix table, lists of an earlier step, slots
+ * reserved and not yet appended) have to be looked up in slot_map.
+ *   slot_map  i32 [n_slots]  out: where the slot's tile is now; -1 for a free slot
+ *   n_live    i32 [1]        out
+ */
+int compact_pool(const scout_problem* p, int32_t* block_table, void* k_pool, void* v_pool,
+                 int64_t n_slots, void* pages, size_t pages_bytes, int32_t* slot_map,
+                 int32_t* n_live, void* stream);
+
+/* Bytes of the plan of a batch with n_prefix prefixes (at most 2048). */
+int scout_prefix_plan_bytes(const scout_problem* p, int32_t n_prefix, size_t* bytes);
+
+/*
+ * The plan of an attention over shared prefixes: which sequences have which prefix,
+ * and how the work is dealt to workgroups.  It holds for every layer and every step
+ * until prefix_of or prefix_len changes; of p it depends on B, Hq, Hkv, d, S and dtype.
+ *   prefix_blocks  row length of the prefixes' table, at most 2^20
+ *   prefix_of      i32 [B]         the sequence's prefix; outside [0, n_prefix): none
+ *   prefix_len     i32 [n_prefix]  tokens, clamped to [0, prefix_blocks * S]
+ *   plan           out: DEVICE, 16-byte aligned, scout_prefix_plan_bytes() bytes
+ */
+int scout_prefix_plan(const scout_problem* p, int32_t n_prefix, int32_t prefix_blocks,
+                      const int32_t* prefix_of, const int32_t* prefix_len, void* plan,
+                      size_t plan_bytes, void* stream);
+
+/*
+ * Decode attention over shared prefixes: for every query head of a sequence with a
+ * prefix, softmax(sm_scale * q.K^T) V over the prefix's tokens that have a slot, a
+ * partial result as sparse_decode_attn returns it, joined with the sequence's own
+ * partial (o_b, m_b, l_b) if there is one: its attention over the tokens behind the
+ * prefix, from sparse_decode_attn or the host.  K and V of a prefix are read once for
+ * all its sequences.
+ *   plan          scout_prefix_plan's, for this p, n_prefix and prefix_blocks (with a plan
+ *                 made for another problem no sequence has a prefix)
+ *   q             e   [B][Hq][d]
+ *   prefix_table  i32 [n_prefix][Hkv][prefix_blocks]  slots; entries outside [0, n_slots)
+ *                 (blocks on the host) are not attended to
+ *   o_b f32 [B][Hq][d], m_b, l_b f32 [B][Hq]  all or none (NULL)
+ *   o, m, l       out: the joined partial, all or none (NULL); may be o_b, m_b, l_b.  It goes on
+ *                 as the host_* of scout_layer_step or scout_attn_finish, a side of
+ *                 merge_partials, or the o_b of a call for further prefixes
+ *   out e [B][Hq][d], lse f32 [B][Hq]  out: the joined result as merge_partials writes
+ *                 it; out may be NULL where o is given, lse always
+ * A sequence without prefix and partial gives o = 0, m = -inf, l = 0, out = 0, lse = -inf.
+ * Products, sums and softmax weights are binary32; bf16 rounds the weights to bf16 before
+ * the value product where only `out` is written, and to two bf16 terms (2^-16) where o is.
+ */
+int shared_prefix_attn(const scout_problem* p, int32_t n_prefix, int32_t prefix_blocks,
+                       const void* plan, size_t plan_bytes, const void* q, const void* k_pool,
+                       const void* v_pool, int64_t n_slots, const int32_t* prefix_table,
+                       const float* o_b, const float* m_b, const float* l_b, float* o, float* m,
+                       float* l, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Tuning knob for measurements: force the attention kernel family, the split
  * count per pair and the workgroup size.  family: 0 = automatic (the matrix
  * cores, for every type and head dim), 1 = generic

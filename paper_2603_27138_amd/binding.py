@@ -28,7 +28,8 @@ STATIC_SCRATCH_BYTES = 8 << 20
 EXPORTS = ["scout_version", "scout_strerror", "scout_workspace_bytes", "build_digests", "append_token", "score_blocks",
            "select_topk", "sparse_decode_attn", "merge_partials", "periodic_recall", "recall_fetch", "recall_scatter",
            "scout_layer_step", "scout_set_attn_mode", "scout_attn_partials", "scout_attn_finish", "scout_select_ahead",
-           "sparse_decode_attn_static"]
+           "sparse_decode_attn_static", "scout_pages_bytes", "scout_pages_init", "reserve_blocks", "fork_sequences", "free_sequences",
+           "compact_pool", "scout_prefix_plan_bytes", "scout_prefix_plan", "shared_prefix_attn"]
 # measurement aids live in a library of their own (include/scout_calib.h)
 CALIB_LIB_PATH = os.path.join(_HERE, "libscout_calib.so")
 CALIB_EXPORTS = ["scout_calib_copy", "scout_calib_read", "scout_calib_gather"]
@@ -82,6 +83,16 @@ def lib():
         L.scout_attn_partials.argtypes = [pp, vp, vp, vp, i64] + [vp] * 4 + [sz, vp]
         L.scout_attn_finish.argtypes = [pp] + [vp] * 6 + [sz, vp]
         L.scout_layer_step.argtypes = [pp, vp, vp, vp, vp, vp, i64] + [vp] * 13 + [sz, vp]
+        i32 = ctypes.c_int32
+        L.scout_pages_bytes.argtypes = [i64, ctypes.POINTER(sz)]
+        L.scout_pages_init.argtypes = [pp, vp, vp, i64, vp, sz, vp]
+        L.reserve_blocks.argtypes = [pp, vp, i64, vp, sz, vp, vp, vp]
+        L.fork_sequences.argtypes = [pp, i32, vp, vp, i32] + [vp] * 5 + [i64, vp, sz, vp, vp]
+        L.free_sequences.argtypes = [pp, i32, vp, vp, vp, i64, vp, sz, vp]
+        L.compact_pool.argtypes = [pp, vp, vp, vp, i64, vp, sz, vp, vp, vp]
+        L.scout_prefix_plan_bytes.argtypes = [pp, i32, ctypes.POINTER(sz)]
+        L.scout_prefix_plan.argtypes = [pp, i32, i32, vp, vp, vp, sz, vp]
+        L.shared_prefix_attn.argtypes = [pp, i32, i32, vp, sz, vp, vp, vp, i64] + [vp] * 9 + [vp, sz, vp]
         for name in EXPORTS:
             if name not in ("scout_strerror",):
                 getattr(L, name).restype = getattr(L, name).restype or ctypes.c_int
@@ -192,6 +203,17 @@ def _ptr_addressable(t: torch.Tensor):
     if isinstance(t, torch.Tensor) and not t.is_cuda:
         (_calls or _load_calls()).used_by_stream(t)
     return ctypes.c_void_p(t.data_ptr())
+
+
+def _ptr_here(t: Optional[torch.Tensor]):
+    """_ptr, of a tensor on the current device: the stream that the call goes to belongs to that one."""
+    p = _ptr(t)
+    assert t is None or t.device.index == torch.cuda.current_device(), "tensors must be on the current device"
+    return p
+
+
+def _bytes(t: torch.Tensor) -> int:
+    return t.numel() * t.element_size()
 
 
 def _stream():
@@ -386,3 +408,96 @@ def layer_step(p: Problem, q, digest, block_table, k_pool, v_pool, n_slots, host
           _ptr(scores), _ptr(sel_all), _ptr(sel_gpu), _ptr(slot_gpu), _ptr(n_gpu),
           _ptr(sel_host), _ptr(n_host), _ptr(out), _ptr(lse), _ptr(ws), ws.numel(),
           _stream())
+
+
+def pages_bytes(n_slots: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check("scout_pages_bytes", lib().scout_pages_bytes(int(n_slots), ctypes.byref(n)))
+    return n.value
+
+
+def alloc_pages(n_slots: int, device="cuda") -> torch.Tensor:
+    """Memory for the pages' state of a pool of n_slots slots: int32, the first n_slots of them the counts of references once
+    pages_init has filled it."""
+    return torch.empty(pages_bytes(n_slots) // 4, dtype=torch.int32, device=device)
+
+
+def pages_init(p: Problem, ctx_len, block_table, n_slots, pages):
+    if _recording is None:
+        return _done("scout_pages_init", (_calls or _load_calls()).pages_init(p, ctx_len, block_table, n_slots, pages))
+    _call("scout_pages_init", lib().scout_pages_init, ctypes.byref(p), _ptr_here(ctx_len), _ptr_here(block_table), int(n_slots),
+          _ptr_here(pages), _bytes(pages), _stream())
+
+
+def reserve_blocks(p: Problem, ctx_len, n_slots, pages, new_slot, n_short):
+    """new_slot: append_token's argument for the token that comes next."""
+    if _recording is None:
+        return _done("reserve_blocks", (_calls or _load_calls()).reserve_blocks(p, ctx_len, n_slots, pages, new_slot, n_short))
+    _call("reserve_blocks", lib().reserve_blocks, ctypes.byref(p), _ptr_here(ctx_len), int(n_slots), _ptr_here(pages), _bytes(pages),
+          _ptr_here(new_slot), _ptr_here(n_short), _stream())
+
+
+def _indices(*lists):
+    """How many sequences the lists name: int32, of one length."""
+    n = lists[0].numel()
+    assert all(t.dtype == torch.int32 and t.numel() == n for t in lists), "sequences are listed in int32, in lists of one length"
+    return n
+
+
+def fork_sequences(p: Problem, src, dst, deep, ctx_len, digest, block_table, k_pool, v_pool, n_slots, pages, status):
+    """Sequence dst[i] becomes a fork of src[i]; deep: with tiles of its own instead of shared ones."""
+    n, deep = _indices(src, dst, status), int(bool(deep))
+    if _recording is None:
+        return _done("fork_sequences", (_calls or _load_calls()).fork_sequences(
+            p, n, src, dst, deep, ctx_len, digest, block_table, k_pool, v_pool, n_slots, pages, status))
+    _call("fork_sequences", lib().fork_sequences, ctypes.byref(p), n, _ptr_here(src), _ptr_here(dst), deep, _ptr_here(ctx_len),
+          _ptr_here(digest), _ptr_here(block_table), _ptr_here(k_pool), _ptr_here(v_pool), int(n_slots), _ptr_here(pages), _bytes(pages),
+          _ptr_here(status), _stream())
+
+
+def free_sequences(p: Problem, seq, ctx_len, block_table, n_slots, pages):
+    n = _indices(seq)
+    if _recording is None:
+        return _done("free_sequences", (_calls or _load_calls()).free_sequences(p, n, seq, ctx_len, block_table, n_slots, pages))
+    _call("free_sequences", lib().free_sequences, ctypes.byref(p), n, _ptr_here(seq), _ptr_here(ctx_len), _ptr_here(block_table),
+          int(n_slots), _ptr_here(pages), _bytes(pages), _stream())
+
+
+def compact_pool(p: Problem, block_table, k_pool, v_pool, n_slots, pages, slot_map, n_live):
+    """slot_map[old slot] = new slot (-1: it was free), for whatever else names slots of this pool."""
+    if _recording is None:
+        return _done("compact_pool", (_calls or _load_calls()).compact_pool(
+            p, block_table, k_pool, v_pool, n_slots, pages, slot_map, n_live))
+    _call("compact_pool", lib().compact_pool, ctypes.byref(p), _ptr_here(block_table), _ptr_here(k_pool), _ptr_here(v_pool), int(n_slots),
+          _ptr_here(pages), _bytes(pages), _ptr_here(slot_map), _ptr_here(n_live), _stream())
+
+
+def prefix_plan_bytes(p: Problem, n_prefix: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check("scout_prefix_plan_bytes", lib().scout_prefix_plan_bytes(ctypes.byref(p), int(n_prefix), ctypes.byref(n)))
+    return n.value
+
+
+def alloc_prefix_plan(p: Problem, n_prefix: int, device="cuda") -> torch.Tensor:
+    return torch.empty(prefix_plan_bytes(p, n_prefix), dtype=torch.uint8, device=device)
+
+
+def prefix_plan(p: Problem, n_prefix, prefix_blocks, prefix_of, prefix_len, plan):
+    """Once for a batch: who has which prefix, and how the attention over them is dealt to workgroups."""
+    if _recording is None:
+        return _done("scout_prefix_plan", (_calls or _load_calls()).prefix_plan(p, n_prefix, prefix_blocks, prefix_of, prefix_len, plan))
+    _call("scout_prefix_plan", lib().scout_prefix_plan, ctypes.byref(p), int(n_prefix), int(prefix_blocks), _ptr_here(prefix_of),
+          _ptr_here(prefix_len), _ptr_here(plan), _bytes(plan), _stream())
+
+
+def shared_prefix_attn(p: Problem, n_prefix, prefix_blocks, plan, q, k_pool, v_pool, n_slots, prefix_table, o_b, m_b, l_b, o, m, l, out,
+                       lse, ws):
+    """Attention over the prefixes, joined with the sequences' own partials o_b, m_b, l_b (or None): the joined partial o, m, l
+    (or None), and the result out (or None) with lse (or None)."""
+    if _recording is None:
+        return _done("shared_prefix_attn", (_calls or _load_calls()).shared_prefix_attn(
+            p, n_prefix, prefix_blocks, plan, q, k_pool, v_pool, n_slots, prefix_table, o_b, m_b, l_b, o, m, l, out, lse, ws))
+    _call("shared_prefix_attn", lib().shared_prefix_attn, ctypes.byref(p), int(n_prefix), int(prefix_blocks), _ptr_here(plan),
+          _bytes(plan), _ptr_here(q), _ptr_here(k_pool), _ptr_here(v_pool), int(n_slots), _ptr_here(prefix_table), _ptr_here(o_b),
+          _ptr_here(m_b), _ptr_here(l_b), _ptr_here(o), _ptr_here(m), _ptr_here(l), _ptr_here(out), _ptr_here(lse), _ptr_here(ws),
+          _bytes(ws), _stream())

@@ -6,6 +6,8 @@
 #include <mutex>
 
 #include "common.h"
+#include "pages.h"
+#include "prefix.h"
 
 namespace scout {
 
@@ -35,6 +37,17 @@ int launch_step(const Dims&, int, const void*, const void*, const int32_t*, cons
                 int32_t*, int32_t*, int32_t*, int32_t*, int32_t*, int32_t*, Partials, Epilogue, hipStream_t);
 int launch_merge(const Dims&, int, const float*, const float*, const float*, const float*,
                  const float*, const float*, void*, float*, hipStream_t);
+
+int launch_pages_init(const Dims&, const Pages&, const int32_t*, const int32_t*, hipStream_t);
+int launch_reserve(const Dims&, const Pages&, const int32_t*, int32_t*, int32_t*, hipStream_t);
+int launch_fork(const Dims&, int, const Pages&, int, const int32_t*, const int32_t*, int, int32_t*, void*, int32_t*, void*, void*,
+                int32_t*, hipStream_t);
+int launch_free(const Dims&, const Pages&, int, const int32_t*, int32_t*, int32_t*, hipStream_t);
+int launch_compact(const Dims&, int, const Pages&, int32_t*, void*, void*, int32_t*, int32_t*, hipStream_t);
+long long prefix_plan_words(const Dims&, int, int);
+int launch_prefix_plan(const Dims&, int, int, int, const int32_t*, const int32_t*, void*, hipStream_t);
+int launch_prefix_attn(const Dims&, int, int, int, void*, const void*, const void*, const void*, long long, const int32_t*, const float*,
+                       const float*, const float*, float*, float*, float*, void*, float*, float*, float*, float*, hipStream_t);
 
 constexpr int kMaxSplit = 64;
 constexpr int kValuHeadsPerWave = 4;
@@ -258,13 +271,34 @@ static size_t static_layout(const Dims& D, const AttnPlan& A, size_t* off_m, siz
   return *off_l + round256(rows * sizeof(float));
 }
 
+// The state of a pool's pages in the caller's buffer.
+static int check_pages(int64_t n_slots, void* pages, size_t bytes, Pages* P) {
+  size_t need;
+  const int rc = scout_pages_bytes(n_slots, &need);
+  if (rc != SCOUT_OK) return rc;
+  if (pages == nullptr || !aligned16(pages) || bytes < need) return SCOUT_EWORKSPACE;
+  *P = Pages::at(pages, n_slots);
+  return SCOUT_OK;
+}
+
+// The plan of shared prefixes in the caller's buffer (which may be null while only its size is asked for).
+static int check_prefixes(const scout_problem* p, int32_t n_prefix, Dims* D, size_t* need) {
+  const int rc = check_problem_kv(p, D);
+  if (rc != SCOUT_OK) return rc;
+  if (n_prefix < 0) return SCOUT_EINVAL;
+  const long long words = n_prefix > kMaxPrefixes ? -1 : prefix_plan_words(*D, p->dtype, n_prefix);
+  if (words < 0) return SCOUT_EUNSUPPORTED;
+  *need = (size_t)words * sizeof(int32_t);
+  return SCOUT_OK;
+}
+
 }  // namespace scout
 
 using namespace scout;
 
 extern "C" {
 
-int scout_version(void) { return 100; }
+int scout_version(void) { return 101; }
 
 const char* scout_strerror(int code) {
   switch (code) {
@@ -604,6 +638,130 @@ int scout_layer_step(const scout_problem* p, const void* q, const void* digest,
   rc = launch_topk(D, scores, block_table, sel_all, sel_gpu, slot_gpu, n_gpu, sel_host, n_host, nullptr, st);
   if (rc != SCOUT_OK) return rc;
   return run_attn(D, p->dtype, A, q, k_pool, v_pool, n_slots, sel_gpu, slot_gpu, n_gpu, ws, L, E, st);
+}
+
+int scout_pages_bytes(int64_t n_slots, size_t* bytes) {
+  if (bytes == nullptr || n_slots < 0) return SCOUT_EINVAL;
+  if (n_slots > (1ll << 29)) return SCOUT_EUNSUPPORTED;
+  *bytes = (size_t)Pages::words(n_slots) * sizeof(int32_t);
+  return SCOUT_OK;
+}
+
+int scout_pages_init(const scout_problem* p, const int32_t* ctx_len, const int32_t* block_table, int64_t n_slots, void* pages,
+                     size_t pages_bytes, void* stream) {
+  Dims D;
+  Pages P;
+  int rc = check_problem_kv(p, &D);
+  if (rc != SCOUT_OK) return rc;
+  if (!ctx_len || !block_table) return SCOUT_EINVAL;
+  rc = check_pages(n_slots, pages, pages_bytes, &P);
+  if (rc != SCOUT_OK) return rc;
+  return launch_pages_init(D, P, ctx_len, block_table, static_cast<hipStream_t>(stream));
+}
+
+int reserve_blocks(const scout_problem* p, const int32_t* ctx_len, int64_t n_slots, void* pages, size_t pages_bytes, int32_t* new_slot,
+                   int32_t* n_short, void* stream) {
+  Dims D;
+  Pages P;
+  int rc = check_problem_kv(p, &D);
+  if (rc != SCOUT_OK) return rc;
+  if (!ctx_len || !new_slot || !n_short) return SCOUT_EINVAL;
+  rc = check_pages(n_slots, pages, pages_bytes, &P);
+  if (rc != SCOUT_OK) return rc;
+  return launch_reserve(D, P, ctx_len, new_slot, n_short, static_cast<hipStream_t>(stream));
+}
+
+int fork_sequences(const scout_problem* p, int32_t n, const int32_t* src, const int32_t* dst, int32_t deep, int32_t* ctx_len,
+                   void* digest, int32_t* block_table, void* k_pool, void* v_pool, int64_t n_slots, void* pages, size_t pages_bytes,
+                   int32_t* status, void* stream) {
+  Dims D;
+  Pages P;
+  int rc = check_problem_kv(p, &D);
+  if (rc != SCOUT_OK) return rc;
+  if (n < 0 || n > D.B || (deep != 0 && deep != 1)) return SCOUT_EINVAL;
+  if ((n > 0 && (!src || !dst || !status)) || !ctx_len || !digest || !block_table) return SCOUT_EINVAL;
+  if (n_slots > 0 && (!k_pool || !v_pool)) return SCOUT_EINVAL;
+  if (!aligned16(digest) || !aligned16(k_pool) || !aligned16(v_pool)) return SCOUT_EINVAL;
+  rc = check_pages(n_slots, pages, pages_bytes, &P);
+  if (rc != SCOUT_OK) return rc;
+  return launch_fork(D, p->dtype, P, n, src, dst, deep, ctx_len, digest, block_table, k_pool, v_pool, status,
+                     static_cast<hipStream_t>(stream));
+}
+
+int free_sequences(const scout_problem* p, int32_t n, const int32_t* seq, int32_t* ctx_len, int32_t* block_table, int64_t n_slots,
+                   void* pages, size_t pages_bytes, void* stream) {
+  Dims D;
+  Pages P;
+  int rc = check_problem_kv(p, &D);
+  if (rc != SCOUT_OK) return rc;
+  if (n < 0 || n > D.B || (n > 0 && !seq) || !ctx_len || !block_table) return SCOUT_EINVAL;
+  rc = check_pages(n_slots, pages, pages_bytes, &P);
+  if (rc != SCOUT_OK) return rc;
+  return launch_free(D, P, n, seq, ctx_len, block_table, static_cast<hipStream_t>(stream));
+}
+
+int compact_pool(const scout_problem* p, int32_t* block_table, void* k_pool, void* v_pool, int64_t n_slots, void* pages,
+                 size_t pages_bytes, int32_t* slot_map, int32_t* n_live, void* stream) {
+  Dims D;
+  Pages P;
+  int rc = check_problem_kv(p, &D);
+  if (rc != SCOUT_OK) return rc;
+  if (!block_table || (n_slots > 0 && !slot_map) || !n_live) return SCOUT_EINVAL;
+  if (n_slots > 0 && (!k_pool || !v_pool)) return SCOUT_EINVAL;
+  if (!aligned16(k_pool) || !aligned16(v_pool)) return SCOUT_EINVAL;
+  rc = check_pages(n_slots, pages, pages_bytes, &P);
+  if (rc != SCOUT_OK) return rc;
+  return launch_compact(D, p->dtype, P, block_table, k_pool, v_pool, slot_map, n_live, static_cast<hipStream_t>(stream));
+}
+
+int scout_prefix_plan_bytes(const scout_problem* p, int32_t n_prefix, size_t* bytes) {
+  Dims D;
+  if (p == nullptr || bytes == nullptr) return SCOUT_EINVAL;
+  scout_problem tmp = *p;  // ctx_len is not needed to size the plan
+  static const int32_t dummy = 0;
+  if (tmp.ctx_len == nullptr) tmp.ctx_len = &dummy;
+  return check_prefixes(&tmp, n_prefix, &D, bytes);
+}
+
+int scout_prefix_plan(const scout_problem* p, int32_t n_prefix, int32_t prefix_blocks, const int32_t* prefix_of,
+                      const int32_t* prefix_len, void* plan, size_t plan_bytes, void* stream) {
+  Dims D;
+  size_t need;
+  const int rc = check_prefixes(p, n_prefix, &D, &need);
+  if (rc != SCOUT_OK) return rc;
+  if (!prefix_of || (n_prefix > 0 && !prefix_len) || prefix_blocks < 1) return SCOUT_EINVAL;
+  if (prefix_blocks > 1 << 20) return SCOUT_EUNSUPPORTED;
+  if (plan == nullptr || !aligned16(plan) || plan_bytes < need) return SCOUT_EWORKSPACE;
+  if (D.B == 0) return SCOUT_OK;
+  return launch_prefix_plan(D, p->dtype, n_prefix, prefix_blocks, prefix_of, prefix_len, plan, static_cast<hipStream_t>(stream));
+}
+
+int shared_prefix_attn(const scout_problem* p, int32_t n_prefix, int32_t prefix_blocks, const void* plan, size_t plan_bytes,
+                       const void* q, const void* k_pool, const void* v_pool, int64_t n_slots, const int32_t* prefix_table,
+                       const float* o_b, const float* m_b, const float* l_b, float* o, float* m, float* l, void* out, float* lse,
+                       void* ws, size_t ws_bytes, void* stream) {
+  Dims D;
+  size_t need;
+  int rc = check_prefixes(p, n_prefix, &D, &need);
+  if (rc != SCOUT_OK) return rc;
+  if (!q || (n_prefix > 0 && !prefix_table) || prefix_blocks < 1 || n_slots < 0) return SCOUT_EINVAL;
+  if (n_slots > 0 && (!k_pool || !v_pool)) return SCOUT_EINVAL;
+  if (prefix_blocks > 1 << 20) return SCOUT_EUNSUPPORTED;
+  const bool any_b = o_b || m_b || l_b, all_b = o_b && m_b && l_b, any = o || m || l, all = o && m && l;
+  if ((any_b && !all_b) || (any && !all) || (!any && !out) || (lse && !out)) return SCOUT_EINVAL;
+  if (!aligned16(q) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(o_b) || !aligned16(o) || !aligned16(out))
+    return SCOUT_EINVAL;
+  if (plan == nullptr || !aligned16(plan) || plan_bytes < need) return SCOUT_EWORKSPACE;
+  WsLayout L;
+  rc = check_ws(D, ws, ws_bytes, &L);
+  if (rc != SCOUT_OK) return rc;
+  if (D.B == 0) return SCOUT_OK;
+  static_assert(kMaxPrefixSplits <= kMaxSplit, "the workspace has room for every split");
+  char* base = static_cast<char*>(ws);
+  return launch_prefix_attn(D, p->dtype, n_prefix, prefix_blocks, const_cast<void*>(plan), q, k_pool, v_pool, n_slots, prefix_table,
+                            o_b, m_b, l_b, o, m, l, out, lse, reinterpret_cast<float*>(base + L.part_o),
+                            reinterpret_cast<float*>(base + L.part_m), reinterpret_cast<float*>(base + L.part_l),
+                            static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

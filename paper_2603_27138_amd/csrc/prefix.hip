@@ -1,0 +1,539 @@
+// Attention of a batch over prefixes that several of its sequences share, computed once for all of them.
+//
+// For every sequence b with a prefix, KV head g and query head h of its group:
+//   x_t = scale q_bh . k_t,  m = max x_t,  l = sum exp(x_t - m),  o = sum exp(x_t - m) v_t / l
+// over the prefix's tokens that have a slot.  Attended to sequence by sequence the prefix's tiles are read once per sequence; here
+// the heads of all its sequences are rows of one product with every tile, which is read once per tile of rows: n sequences read
+// 1/n of the bytes, and beyond some 190 rows a KV head (1.15 PFLOP/s over 6.2 TB/s) it is the matrix instructions that bound it.
+//
+// prefix_plan_kernel deals the work once for a batch (the lengths of prefixes and who has them do not change with the layer);
+// prefix_attn_kernel leaves a partial per row and split; prefix_combine_kernel folds them, with the sequence's own partial.
+#include "attn_unit.h"
+#include "prefix.h"
+
+namespace scout {
+
+// ---------------------------------------------------------------- the plan
+
+constexpr int kPlanThreads = 1024;
+
+struct PrefixStamp {
+  int32_t w[PrefixPlan::kStampWords];
+};
+
+// Splits that a prefix of len tokens is cut into where a chunk has `chunk` tokens.
+__device__ __forceinline__ int splits_of(int len, int chunk) { return (len + chunk - 1) / chunk; }
+__device__ __forceinline__ int round_up(int x, int to) { return (x + to - 1) / to * to; }
+
+__global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PrefixPlan P, PrefixStamp stamp, PrefixShape shape, int B, int Hkv,
+                                                                   int G, int n_prefix, int max_tokens,
+                                                                   const int32_t* __restrict__ prefix_of,
+                                                                   const int32_t* __restrict__ prefix_len) {
+  // of each prefix: its sequences, how many of them have been put in the list, where its part of the list starts, its tokens, its
+  // first item
+  __shared__ int count[kMaxPrefixes], placed[kMaxPrefixes], first[kMaxPrefixes], len[kMaxPrefixes], base[kMaxPrefixes + 1];
+  __shared__ long long cost[kMaxPrefixSplits];
+  __shared__ int chunk_lds, longest_lds;
+  const int t = threadIdx.x;
+  for (int p = t; p < n_prefix; p += kPlanThreads) {
+    const int n = prefix_len[p];
+    len[p] = n < 0 ? 0 : n > max_tokens ? max_tokens : n;
+    count[p] = placed[p] = 0;
+  }
+  if (t == 0) longest_lds = 0;
+  __syncthreads();
+  for (int b = t; b < B; b += kPlanThreads) {
+    const int p = prefix_of[b];
+    if (p >= 0 && p < n_prefix) atomicAdd(&count[p], 1);
+  }
+  __syncthreads();
+  for (int p = t; p < n_prefix; p += kPlanThreads) {
+    if (count[p] == 0) len[p] = 0;  // nobody has it
+    atomicMax(&longest_lds, len[p]);
+  }
+  if (t == 0) {
+    int at = 0;
+    for (int p = 0; p < n_prefix; ++p) {
+      first[p] = at;
+      at += count[p];
+    }
+  }
+  __syncthreads();
+  const int longest = longest_lds;
+  auto tiles_of = [&](int p) { return (int)(((long long)count[p] * G + shape.tile_rows - 1) / shape.tile_rows); };
+  // How long a chunk is: candidate c cuts the longest prefix c + 1 ways.  shape.slots workgroups run at a time, so a candidate costs as
+  // many rounds as its items fill, each as long as a chunk and what an item costs beyond its tokens.
+  auto chunk_of = [&](int c) {
+    const int n = round_up((longest + c) / (c + 1), shape.granule);
+    return n > shape.granule ? n : shape.granule;
+  };
+  if (t < kMaxPrefixSplits) {
+    const int c = chunk_of(t);
+    long long items = 0;
+    for (int p = 0; p < n_prefix; ++p) items += (long long)tiles_of(p) * Hkv * splits_of(len[p], c);
+    const long long rounds = (items + shape.slots - 1) / shape.slots;
+    cost[t] = items > P.max_items ? 1ll << 62 : rounds * (c + shape.head_cost);
+  }
+  __syncthreads();
+  if (t == 0) {
+    int best = 0;  // without splits the items always fit
+    for (int c = 1; c < kMaxPrefixSplits; ++c)
+      if (cost[c] < cost[best]) best = c;
+    const int chunk = chunk_of(best);
+    int at = 0, most = 1;
+    for (int p = 0; p < n_prefix; ++p) {
+      const int s = splits_of(len[p], chunk);
+      base[p] = at;
+      at += tiles_of(p) * Hkv * s;
+      most = s > most ? s : most;
+    }
+    base[n_prefix] = at;
+    chunk_lds = chunk;
+    P.head[0] = at;
+    P.head[1] = most;
+  }
+  if (t < PrefixPlan::kStampWords) P.stamp[t] = stamp.w[t];
+  __syncthreads();
+  const int chunk = chunk_lds;
+  for (int b = t; b < B; b += kPlanThreads) {
+    const int p = prefix_of[b];
+    const bool has = p >= 0 && p < n_prefix;
+    P.splits[b] = has ? splits_of(len[p], chunk) : 0;
+    // in whichever order the additions come: a row's result does not depend on the rows beside it
+    if (has) P.member[first[p] + atomicAdd(&placed[p], 1)] = b;
+  }
+  for (int i = t; i < base[n_prefix]; i += kPlanThreads) {
+    int p = 0, hi = n_prefix - 1;  // the last prefix whose items start at i or before: the one that i belongs to
+    while (p < hi) {
+      const int mid = (p + hi + 1) >> 1;
+      if (base[mid] <= i) p = mid;
+      else hi = mid - 1;
+    }
+    const int s = splits_of(len[p], chunk), units = Hkv * s, tiles = tiles_of(p);
+    // A unit (split, KV head) has a workgroup per tile of rows, and all of them read the same tokens: their numbers are eight apart,
+    // so that they run on the same XCD and find in its L2 what one of them has read.
+    const int k = i - base[p], full = units / 8 * 8 * tiles;
+    int unit, tile;
+    if (k < full) {
+      unit = k / (8 * tiles) * 8 + k % 8;
+      tile = k / 8 % tiles;
+    } else {
+      unit = units / 8 * 8 + (k - full) % (units % 8);
+      tile = (k - full) / (units % 8);
+    }
+    const int split = unit / Hkv, rows = count[p] * G - tile * shape.tile_rows;
+    const int even = round_up((len[p] + s - 1) / s, shape.granule);  // at most the chunk: no split is empty
+    PrefixItem it;
+    it.prefix = p;
+    it.head = unit % Hkv;
+    it.member0 = first[p];
+    it.row0 = tile * shape.tile_rows;
+    it.rows = rows < shape.tile_rows ? rows : shape.tile_rows;
+    it.tok0 = split * even;
+    it.tok1 = it.tok0 + even < len[p] ? it.tok0 + even : len[p];
+    it.split = split;
+    P.item[i] = it;
+  }
+}
+
+// ---------------------------------------------------------------- the attention
+
+// What a launch works on.
+struct PrefixWork {
+  int B, Hq, Hkv, G, S, s_shift, tile_stride, prefix_blocks, n_prefix;
+  uint32_t g_magic;  // ceil(2^32 / G); 0 for G = 1
+  float scale2;      // softmax scale in base-2 units
+  long long n_slots;
+  const void *q, *k_pool, *v_pool;
+  const int32_t* table;  // [n_prefix][Hkv][prefix_blocks]
+  float *po, *pm, *pl;   // partials [B * Hq][splits of the plan]: unnormalised sums, maximum in base-2 units, sum
+};
+
+__device__ __forceinline__ bool made_for(const PrefixPlan& P, const PrefixStamp& stamp) {
+  bool same = true;
+#pragma unroll
+  for (int i = 0; i < PrefixPlan::kStampWords; ++i) same &= P.stamp[i] == stamp.w[i];
+  return same;
+}
+
+// The query row, of all [B * Hq], that row r of an item is.
+__device__ __forceinline__ int query_row(const PrefixPlan& P, const PrefixWork& W, const PrefixItem& it, int r) {
+  const uint32_t rr = (uint32_t)(it.row0 + r);
+  const uint32_t m = W.g_magic ? __umulhi(rr, W.g_magic) : rr;
+  return P.member[it.member0 + (int)m] * W.Hq + it.head * W.G + (int)(rr - m * W.G);
+}
+
+constexpr int kNarrowWaves = 8;
+
+// Up to 64 rows.  The waves of a workgroup take units of 16 tokens in turn (wave v: v, v + 8, ...); K and V rows go from memory into
+// MFMA operand registers, and NQ column tiles of 16 rows are multiplied with them there (layout: see attn_unit.h).  Bound by memory: a unit is
+// 8 KiB at bf16, d = 128.  The waves fold through LDS.
+// TERMS: bf16 terms of a softmax weight in the second product (bf16 only).  One where the result leaves as bf16 (half a step of 2^-8 of each weight,
+// as much as the output's own rounding); two where it leaves in binary32 (2^-16).  The sum l always has the weights as they are.
+template <int DT, int DH, int NQ, int TERMS>
+__global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(PrefixPlan P, PrefixStamp stamp, PrefixWork W) {
+  using L = Tile<DT, DH>;
+  constexpr int WAVES = kNarrowWaves, ROW = DH + 4;
+  __shared__ float smem[WAVES * (16 * ROW + 32)];
+  if (!made_for(P, stamp) || (int)blockIdx.x >= P.head[0]) return;
+  const PrefixItem it = P.item[blockIdx.x];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), ln = lane & 15, kg = lane >> 4;
+  const int ush = W.s_shift - 4;
+  const int u0 = it.tok0 / kUnitTokens + wave, u1 = (it.tok1 + kUnitTokens - 1) / kUnitTokens;
+  const int32_t* row = W.table + ((size_t)it.prefix * W.Hkv + it.head) * W.prefix_blocks;
+  // lane j: the slot of this wave's unit number j, 64 units at a time
+  auto fetch_slots = [&](int u) {
+    const int mine = u + lane * WAVES;
+    return mine < u1 ? row[mine >> ush] : -1;
+  };
+  int slots = fetch_slots(u0), slots_next = -1;
+  QRegs<DT, DH> qreg[NQ];
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+    const int r = t * 16 + ln;
+    const bool real = r < it.rows;
+    const char* at = static_cast<const char*>(W.q) + (size_t)query_row(P, W, it, real ? r : it.rows - 1) * L::ROWB + kg * 16;
+#pragma unroll
+    for (int s = 0; s < L::KL; ++s) {
+      qreg[t][s] = *reinterpret_cast<const u32x4*>(at + s * 64);
+      qreg[t][s] &= real ? 0xffffffffu : 0u;
+    }
+  }
+  f32x4 acc[NQ][L::NR];
+  float m[NQ], l[NQ];
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+#pragma unroll
+    for (int r = 0; r < L::NR; ++r) acc[t][r] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    m[t] = -INFINITY;
+    l[t] = 0.0f;
+  }
+  auto entry = [&](int j, int u) {
+    Entry e{0, 0};
+    const long long slot = __builtin_amdgcn_readlane(slots, j);
+    if (u < u1 && slot >= 0 && slot < W.n_slots) {
+      const int left = it.tok1 - u * kUnitTokens;
+      e.valid = left < kUnitTokens ? left : kUnitTokens;
+      e.elem_off = (size_t)slot * W.tile_stride + (size_t)(u & ((1 << ush) - 1)) * kUnitTokens * DH;
+    }
+    return e;
+  };
+  UnitRegs<DT, DH> T;
+  Entry e = entry(0, u0);
+  issue_unit<DT, DH>(T, W.k_pool, W.v_pool, e, ln, kg);
+  slots_next = fetch_slots(u0 + kWave * WAVES);
+  int j = 1;
+  for (int u = u0; u < u1; u += WAVES) {
+    if (j == kWave) {
+      slots = slots_next;
+      slots_next = fetch_slots(u + WAVES + kWave * WAVES);
+      j = 0;
+    }
+    const Entry next = entry(j++, u + WAVES);
+    if (e.valid > 0) {  // wave-uniform
+      if (e.valid < kUnitTokens) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (4 * kg + i >= e.valid) {
+#pragma unroll
+            for (int c = 0; c < L::VC; ++c) T.v[i][c] = (u32x4){0, 0, 0, 0};
+          }
+      }
+#pragma unroll
+      for (int t = 0; t < NQ; ++t) {
+        f32x4 st = (f32x4){0.f, 0.f, 0.f, 0.f};
+        if constexpr (DT == SCOUT_BF16) {
+#pragma unroll
+          for (int s = 0; s < L::KL; ++s)
+            st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(T.k[s]), as_bf16x8(qreg[t][s]), st, 0, 0, 0);
+        } else {
+          // chains of 8 channels, joined pairwise: the rounding of one chain over all of them is what the outputs' error would show
+          f32x4 part[L::KL];
+#pragma unroll
+          for (int s = 0; s < L::KL; ++s) {
+            f32x4 half[2];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              if (c % 2 == 0) half[c / 2] = (f32x4){0.f, 0.f, 0.f, 0.f};
+              half[c / 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(T.k[s][c]), __uint_as_float(qreg[t][s][c]), half[c / 2], 0, 0, 0);
+            }
+            part[s] = half[0] + half[1];
+          }
+#pragma unroll
+          for (int n = L::KL / 2; n > 0; n /= 2)
+#pragma unroll
+            for (int s = 0; s < n; ++s) part[s] += part[s + n];
+          st = part[0];
+        }
+        // Scaled here, in front of the branch: a product's result is first read in the block that the product stands in.  Where the
+        // first reader was the maximum behind the branch, the compiler (ROCm 7.2) put no wait states in front of it, and it read the
+        // registers' old contents.
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = st[i] * W.scale2;
+        if (e.valid < kUnitTokens) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (4 * kg + i >= e.valid) x[i] = -INFINITY;
+        }
+        const float bm = max_xor32(max_xor16(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))));
+        const float m_new = fmaxf(m[t], bm);
+        const float m_sub = m_new == -INFINITY ? 0.0f : m_new;
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = fast_exp2(x[i] - m_sub);
+        if (__ballot(m_new != m[t]) != 0) {
+          const float alpha = exp2_diff(m[t], m_new);
+          l[t] *= alpha;
+#pragma unroll
+          for (int r = 0; r < L::NR; ++r) acc[t][r] *= alpha;
+          m[t] = m_new;
+        }
+        l[t] += (p[0] + p[1]) + (p[2] + p[3]);
+        if constexpr (DT == SCOUT_BF16) {
+          s16x4 term[TERMS];
+#pragma unroll
+          for (int n = 0; n < TERMS; ++n) {
+            if (n + 1 < TERMS) {  // cut, not rounded: what is left is not negative
+              uint32_t hi[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                hi[i] = __float_as_uint(p[i]) & 0xffff0000u;
+                p[i] -= __uint_as_float(hi[i]);
+              }
+              term[n] = __builtin_bit_cast(s16x4, (uint2){pack_halves(hi[0], hi[1], 1), pack_halves(hi[2], hi[3], 1)});
+            } else {
+              if (TERMS > 1) {  // nothing left times an infinite value is not NaN
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[i] = fmaxf(p[i], 0x1p-126f);
+              }
+              term[n] = __builtin_bit_cast(s16x4, (uint2){cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3])});
+            }
+          }
+#pragma unroll
+          for (int r = 0; r < L::NR; ++r) {
+            const uint32_t a01 = pack_halves(T.v[0][0][r >> 1], T.v[1][0][r >> 1], r & 1);
+            const uint32_t a23 = pack_halves(T.v[2][0][r >> 1], T.v[3][0][r >> 1], r & 1);
+            const s16x4 v = __builtin_bit_cast(s16x4, (uint2){a01, a23});
+#pragma unroll
+            for (int n = TERMS - 1; n >= 0; --n) acc[t][r] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, term[n], acc[t][r], 0, 0, 0);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < L::NR; ++r)
+              acc[t][r] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(T.v[i][r / 4][r % 4]), p[i], acc[t][r], 0, 0, 0);
+        }
+      }
+    }
+    e = next;
+    issue_unit<DT, DH>(T, W.k_pool, W.v_pool, e, ln, kg);
+  }
+  // the waves' partials of 16 rows at a time
+  const int stride = P.head[1];
+  constexpr int AREA = 16 * ROW + 32, Q = DH / 2;
+#pragma unroll
+  for (int t = 0; t < NQ; ++t) {
+    if (t * 16 >= it.rows) break;
+    const float lsum = sum_xor32(sum_xor16(l[t]));
+    float* wo = smem + wave * AREA;
+    if (t > 0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int r = 0; r < L::NR; r += 4)
+        *reinterpret_cast<float4*>(wo + ln * ROW + L::channel(r, 4 * kg + i)) =
+            make_float4(acc[t][r][i], acc[t][r + 1][i], acc[t][r + 2][i], acc[t][r + 3][i]);
+    if (kg == 0) {
+      wo[16 * ROW + ln] = m[t];
+      wo[16 * ROW + 16 + ln] = lsum;
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < 16 * Q; x += WAVES * kWave) {
+      const int h = x / Q, c = (x % Q) * 2;
+      if (t * 16 + h >= it.rows) continue;
+      float M = -INFINITY, sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) M = fmaxf(M, smem[w * AREA + 16 * ROW + h]);
+      f32x2 o = (f32x2){0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const float* base = smem + w * AREA;
+        const float f = exp2_diff(base[16 * ROW + h], M);
+        const f32x2 y = *reinterpret_cast<const f32x2*>(base + h * ROW + c);
+        o[0] += f * y[0];
+        o[1] += f * y[1];
+        sum += f * base[16 * ROW + 16 + h];
+      }
+      const size_t at = (size_t)query_row(P, W, it, t * 16 + h) * stride + it.split;
+      *reinterpret_cast<f32x2*>(W.po + at * DH + c) = o;
+      if (c == 0) {
+        W.pm[at] = M;
+        W.pl[at] = sum;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- the splits, and the sequence's own partial
+
+struct PrefixOut {
+  const float *o_b, *m_b, *l_b;  // the other partial, or all null
+  float *o, *m, *l;              // the joined partial, or all null
+  void* out;                     // the joined result, or null
+  float* lse;                    // or null
+};
+
+// A wave per query row: lane s holds the maximum and the sum of split s.
+template <int DT, int DH>
+__global__ __launch_bounds__(256) void prefix_combine_kernel(PrefixPlan P, PrefixStamp stamp, PrefixWork W, PrefixOut E) {
+  constexpr int N = DH / kWave;  // channels per lane
+  typedef typename Channels<N>::f chans;
+  const int lane = lane_id(), row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  if (row >= W.B * W.Hq) return;
+  const int c = lane * N;
+  float mb = -INFINITY, lb = 0.0f;
+  chans ob{};
+  if (E.o_b != nullptr) {
+    mb = E.m_b[row];
+    lb = E.l_b[row];
+    ob = *reinterpret_cast<const typename Channels<N>::f_any*>(E.o_b + (size_t)row * DH + c);
+  }
+  int n = 0, stride = 1;
+  if (made_for(P, stamp)) {
+    n = P.splits[row / W.Hq];
+    stride = P.head[1];
+  }
+  const size_t at = (size_t)row * stride;
+  float ms = lane < n ? W.pm[at + lane] : -INFINITY;
+  float ls = lane < n ? W.pl[at + lane] : 0.0f;
+  float M = ms;
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) M = fmaxf(M, __shfl_xor(M, s));
+  const float f = exp2_diff(ms, M);
+  ls *= f;
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) ls += __shfl_xor(ls, s);
+  chans o{};
+  for (int s0 = 0; s0 < n; s0 += 4) {
+    chans x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      x[u] = *reinterpret_cast<const chans*>(W.po + (at + (s0 + u < n ? s0 + u : n - 1)) * DH + c);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (s0 + u < n) {
+        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s0 + u));
+        if (w > 0.0f) o += w * x[u];  // a split without tokens has no weight
+      }
+  }
+  // The two partials as one.  A side without tokens (sum zero) has no weight, whatever its other numbers; a sum that is NaN
+  // stays one.
+  const float ma = M * kLn2;
+  const float top = fmaxf(ls == 0.0f ? -INFINITY : ma, lb == 0.0f ? -INFINITY : mb);
+  const float ea = ls == 0.0f ? 0.0f : expf(ma - top), wb = lb == 0.0f ? 0.0f : lb * expf(mb - top);
+  const float sum = ls * ea + wb;
+  chans r{};
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    float y = ea == 0.0f ? 0.0f : ea * o[i];  // o is not divided by its sum
+    if (wb != 0.0f) y += wb * ob[i];
+    r[i] = sum == 0.0f ? 0.0f : y / sum;
+  }
+  const size_t to = (size_t)row * DH + c;
+  if (E.out != nullptr) {
+    if constexpr (DT == SCOUT_BF16) {
+      typename Channels<N>::h w;
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = (uint16_t)f32_to_bf16_bits(r[i]);
+      *reinterpret_cast<typename Channels<N>::h_any*>(static_cast<uint16_t*>(E.out) + to) = w;
+    } else {
+      *reinterpret_cast<typename Channels<N>::f_any*>(static_cast<float*>(E.out) + to) = r;
+    }
+    if (E.lse != nullptr && lane == 0) E.lse[row] = sum == 0.0f ? -INFINITY : top + logf(sum);
+  }
+  if (E.o != nullptr) {
+    *reinterpret_cast<typename Channels<N>::f_any*>(E.o + to) = r;
+    if (lane == 0) {
+      E.m[row] = top;
+      E.l[row] = sum;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- launches
+
+// How the work of a batch is dealt: by the rows that a prefix has on average (the rows of a prefix with more are several tiles).
+static PrefixShape prefix_shape(const Dims& D, int dtype, int n_prefix) {
+  const long long rows = ((long long)D.B * D.G + n_prefix - 1) / (n_prefix > 0 ? n_prefix : 1);
+  const int most = dtype == SCOUT_BF16 ? 64 : 32;  // fp32: twice the registers per row
+  PrefixShape s;
+  s.tile_rows = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : 64;
+  s.granule = 64;
+  s.slots = 256;
+  s.head_cost = 256;
+  return s;
+}
+
+static int max_items(const Dims& D, const PrefixShape& s, int n_prefix) {
+  const long long tiles = (long long)D.B * D.G / s.tile_rows + n_prefix;
+  const long long n = tiles * D.Hkv + 2 * s.slots;
+  return n > (1 << 28) ? -1 : (int)n;
+}
+
+static PrefixStamp prefix_stamp(const Dims& D, int dtype, const PrefixShape& s, int n_prefix, int prefix_blocks, int items) {
+  return PrefixStamp{{0x50726669, D.B, D.Hq, D.Hkv, D.d, D.S, dtype, n_prefix, prefix_blocks, s.tile_rows, s.granule, items}};
+}
+
+long long prefix_plan_words(const Dims& D, int dtype, int n_prefix) {
+  const int items = max_items(D, prefix_shape(D, dtype, n_prefix), n_prefix);
+  return items < 0 ? -1 : PrefixPlan::words(D.B, items);
+}
+
+int launch_prefix_plan(const Dims& D, int dtype, int n_prefix, int prefix_blocks, const int32_t* prefix_of, const int32_t* prefix_len,
+                       void* plan, hipStream_t st) {
+  const PrefixShape s = prefix_shape(D, dtype, n_prefix);
+  const int items = max_items(D, s, n_prefix);
+  hipLaunchKernelGGL(prefix_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, PrefixPlan::at(plan, D.B, items),
+                     prefix_stamp(D, dtype, s, n_prefix, prefix_blocks, items), s, D.B, D.Hkv, D.G, n_prefix, prefix_blocks * D.S,
+                     prefix_of, prefix_len);
+  return hipGetLastError() == hipSuccess ? SCOUT_OK : SCOUT_EHIP;
+}
+
+template <int DT, int DH, int TERMS>
+static void launch_narrow(int nq, int grid, const PrefixPlan& P, const PrefixStamp& stamp, const PrefixWork& W, hipStream_t st) {
+  const dim3 block(kNarrowWaves * kWave);
+  if (nq == 1) hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 1, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
+  else if (nq == 2 || DT == SCOUT_F32) hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 2, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
+  else if constexpr (DT == SCOUT_BF16)
+    hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 4, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
+}
+
+template <int DT, int DH>
+static void launch_all(const Dims& D, const PrefixShape& s, int items, const PrefixPlan& P, const PrefixStamp& stamp, const PrefixWork& W,
+                       const PrefixOut& E, hipStream_t st) {
+  const int nq = s.tile_rows / 16;
+  if (DT == SCOUT_BF16 && E.o != nullptr) launch_narrow<DT, DH, 2>(nq, items, P, stamp, W, st);
+  else launch_narrow<DT, DH, 1>(nq, items, P, stamp, W, st);
+  hipLaunchKernelGGL((prefix_combine_kernel<DT, DH>), dim3((D.B * D.Hq + 3) / 4), dim3(256), 0, st, P, stamp, W, E);
+}
+
+int launch_prefix_attn(const Dims& D, int dtype, int n_prefix, int prefix_blocks, void* plan, const void* q, const void* k_pool,
+                       const void* v_pool, long long n_slots, const int32_t* table, const float* o_b, const float* m_b, const float* l_b,
+                       float* o, float* m, float* l, void* out, float* lse, float* po, float* pm, float* pl, hipStream_t st) {
+  const PrefixShape s = prefix_shape(D, dtype, n_prefix);
+  const int items = max_items(D, s, n_prefix);
+  const PrefixPlan P = PrefixPlan::at(plan, D.B, items);
+  const PrefixStamp stamp = prefix_stamp(D, dtype, s, n_prefix, prefix_blocks, items);
+  const PrefixWork W{D.B, D.Hq, D.Hkv, D.G, D.S, D.s_shift, D.tile_stride, prefix_blocks, n_prefix,
+                     D.G > 1 ? (uint32_t)(((1ull << 32) + D.G - 1) / D.G) : 0, D.sm_scale * kLog2e, n_slots, q, k_pool, v_pool, table, po,
+                     pm, pl};
+  const PrefixOut E{o_b, m_b, l_b, o, m, l, out, lse};
+  if (D.B == 0) return SCOUT_OK;
+  if (dtype == SCOUT_BF16) D.d == 128 ? launch_all<SCOUT_BF16, 128>(D, s, items, P, stamp, W, E, st) : launch_all<SCOUT_BF16, 64>(D, s, items, P, stamp, W, E, st);
+  else D.d == 128 ? launch_all<SCOUT_F32, 128>(D, s, items, P, stamp, W, E, st) : launch_all<SCOUT_F32, 64>(D, s, items, P, stamp, W, E, st);
+  return hipGetLastError() == hipSuccess ? SCOUT_OK : SCOUT_EHIP;
+}
+
+}  // namespace scout

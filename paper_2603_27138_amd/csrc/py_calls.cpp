@@ -52,6 +52,7 @@ struct Args {
   bool ok = true;
   Py_buffer problem{};
   bool have_problem = false;
+  int device = -1;  // where device tensors have to be; -1: not looked at
 
   Args(const char* fn_, PyObject* const* a_, Py_ssize_t n_, Py_ssize_t want) : fn(fn_), a(a_), n(n_) {
     if (n != want) {
@@ -64,6 +65,11 @@ struct Args {
   }
   Args(const Args&) = delete;
   Args& operator=(const Args&) = delete;
+
+  // from here on device tensors have to be on the current device, whose stream the call goes to
+  void here() {
+    if (ok) device = at::accelerator::getDeviceIndex();
+  }
 
   PyObject* next() { return a[at++]; }
 
@@ -104,6 +110,11 @@ struct Args {
       ok = false;
       return nullptr;
     }
+    if (device >= 0 && t.is_cuda() && t.get_device() != device) {
+      PyErr_SetString(PyExc_AssertionError, "tensors must be on the current device");
+      ok = false;
+      return nullptr;
+    }
     if (!t.is_cuda()) used_by_stream(t);
     return t.data_ptr();
   }
@@ -134,6 +145,23 @@ struct Args {
     Py_XDECREF(n);
     if (PyErr_Occurred()) ok = false;
     return ws;
+  }
+  // a buffer whose size goes with it, whatever its elements are
+  void* buffer(size_t* bytes) {
+    *bytes = 0;
+    if (!ok) return nullptr;
+    PyObject* const o = a[at];
+    void* const address = workspace(bytes);
+    if (!ok) return nullptr;
+    if (THPVariable_CheckExact(o)) {
+      *bytes *= THPVariable_Unpack(o).element_size();
+      return address;
+    }
+    PyObject* const size = PyObject_CallMethod(o, "element_size", nullptr);
+    *bytes *= size == nullptr ? 0 : (size_t)PyLong_AsUnsignedLongLongMask(size);
+    Py_XDECREF(size);
+    if (PyErr_Occurred()) ok = false;
+    return address;
   }
   int64_t integer() {
     if (!ok) return 0;
@@ -169,6 +197,13 @@ struct Table {
   decltype(&::recall_fetch) recall_fetch;
   decltype(&::recall_scatter) recall_scatter;
   decltype(&::scout_layer_step) scout_layer_step;
+  decltype(&::scout_pages_init) scout_pages_init;
+  decltype(&::reserve_blocks) reserve_blocks;
+  decltype(&::fork_sequences) fork_sequences;
+  decltype(&::free_sequences) free_sequences;
+  decltype(&::compact_pool) compact_pool;
+  decltype(&::scout_prefix_plan) scout_prefix_plan;
+  decltype(&::shared_prefix_attn) shared_prefix_attn;
 } T;
 
 // Every function returns the library's code; binding.py turns a negative one into ScoutError.
@@ -357,6 +392,103 @@ PyObject* py_layer_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                   n_gpu, sel_host, n_host, out, lse, ws, nws, st));
 }
 
+PyObject* py_pages_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args A("scout_pages_init", a, n, 5);
+  const auto* p = A.prob();
+  A.here();
+  i32 *ctx = A.dev<i32>(), *table = A.dev<i32>();
+  const int64_t slots = A.integer();
+  size_t npages;
+  void* pages = A.buffer(&npages);
+  SCOUT_RETURN(T.scout_pages_init(p, ctx, table, slots, pages, npages, st));
+}
+
+PyObject* py_reserve_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args A("reserve_blocks", a, n, 6);
+  const auto* p = A.prob();
+  A.here();
+  i32* ctx = A.dev<i32>();
+  const int64_t slots = A.integer();
+  size_t npages;
+  void* pages = A.buffer(&npages);
+  i32 *new_slot = A.dev<i32>(), *n_short = A.dev<i32>();
+  SCOUT_RETURN(T.reserve_blocks(p, ctx, slots, pages, npages, new_slot, n_short, st));
+}
+
+PyObject* py_fork_sequences(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args A("fork_sequences", a, n, 13);
+  const auto* p = A.prob();
+  A.here();
+  const int64_t count = A.integer();
+  i32 *src = A.dev<i32>(), *dst = A.dev<i32>();
+  const int64_t deep = A.integer();
+  i32* ctx = A.dev<i32>();
+  void* digest = A.dev();
+  i32* table = A.dev<i32>();
+  void *kp = A.dev(), *vp = A.dev();
+  const int64_t slots = A.integer();
+  size_t npages;
+  void* pages = A.buffer(&npages);
+  i32* status = A.dev<i32>();
+  SCOUT_RETURN(T.fork_sequences(p, (i32)count, src, dst, (i32)deep, ctx, digest, table, kp, vp, slots, pages, npages, status, st));
+}
+
+PyObject* py_free_sequences(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args A("free_sequences", a, n, 7);
+  const auto* p = A.prob();
+  A.here();
+  const int64_t count = A.integer();
+  i32 *seq = A.dev<i32>(), *ctx = A.dev<i32>(), *table = A.dev<i32>();
+  const int64_t slots = A.integer();
+  size_t npages;
+  void* pages = A.buffer(&npages);
+  SCOUT_RETURN(T.free_sequences(p, (i32)count, seq, ctx, table, slots, pages, npages, st));
+}
+
+PyObject* py_compact_pool(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args A("compact_pool", a, n, 8);
+  const auto* p = A.prob();
+  A.here();
+  i32* table = A.dev<i32>();
+  void *kp = A.dev(), *vp = A.dev();
+  const int64_t slots = A.integer();
+  size_t npages;
+  void* pages = A.buffer(&npages);
+  i32 *slot_map = A.dev<i32>(), *n_live = A.dev<i32>();
+  SCOUT_RETURN(T.compact_pool(p, table, kp, vp, slots, pages, npages, slot_map, n_live, st));
+}
+
+PyObject* py_prefix_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args A("scout_prefix_plan", a, n, 6);
+  const auto* p = A.prob();
+  A.here();
+  const int64_t prefixes = A.integer(), blocks = A.integer();
+  i32 *of = A.dev<i32>(), *len = A.dev<i32>();
+  size_t nplan;
+  void* plan = A.buffer(&nplan);
+  SCOUT_RETURN(T.scout_prefix_plan(p, (i32)prefixes, (i32)blocks, of, len, plan, nplan, st));
+}
+
+PyObject* py_shared_prefix_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Args A("shared_prefix_attn", a, n, 18);
+  const auto* p = A.prob();
+  A.here();
+  const int64_t prefixes = A.integer(), blocks = A.integer();
+  size_t nplan;
+  void* plan = A.buffer(&nplan);
+  void *q = A.dev(), *kp = A.dev(), *vp = A.dev();
+  const int64_t slots = A.integer();
+  i32* table = A.dev<i32>();
+  float *ob = A.dev<float>(), *mb = A.dev<float>(), *lb = A.dev<float>(), *o = A.dev<float>(), *m = A.dev<float>(),
+        *l = A.dev<float>();
+  void* out = A.dev();
+  float* lse = A.dev<float>();
+  size_t nws;
+  void* ws = A.buffer(&nws);
+  SCOUT_RETURN(T.shared_prefix_attn(p, (i32)prefixes, (i32)blocks, plan, nplan, q, kp, vp, slots, table, ob, mb, lb, o, m, l, out,
+                                    lse, ws, nws, st));
+}
+
 // bind(addresses by name, Problem, _ptr, _ptr_addressable, _stream): where the loaded library has its entry points, and what
 // binding.py makes of an argument.
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -389,6 +521,13 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   SCOUT_BIND(recall_fetch);
   SCOUT_BIND(recall_scatter);
   SCOUT_BIND(scout_layer_step);
+  SCOUT_BIND(scout_pages_init);
+  SCOUT_BIND(reserve_blocks);
+  SCOUT_BIND(fork_sequences);
+  SCOUT_BIND(free_sequences);
+  SCOUT_BIND(compact_pool);
+  SCOUT_BIND(scout_prefix_plan);
+  SCOUT_BIND(shared_prefix_attn);
   PyObject** const kept[] = {&py.problem, &py.ptr, &py.ptr_addressable, &py.stream};
   for (int i = 0; i < 4; ++i) {
     Py_INCREF(a[i + 1]);
@@ -438,6 +577,13 @@ PyMethodDef methods[] = {
     SCOUT_METHOD(recall_fetch),
     SCOUT_METHOD(recall_scatter),
     SCOUT_METHOD(layer_step),
+    SCOUT_METHOD(pages_init),
+    SCOUT_METHOD(reserve_blocks),
+    SCOUT_METHOD(fork_sequences),
+    SCOUT_METHOD(free_sequences),
+    SCOUT_METHOD(compact_pool),
+    SCOUT_METHOD(prefix_plan),
+    SCOUT_METHOD(shared_prefix_attn),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
