@@ -8,10 +8,14 @@
 //
 // prefix_plan_kernel deals the work once for a batch (the lengths of prefixes and who has them do not change with the layer);
 // prefix_attn_kernel leaves a partial per row and split; prefix_combine_kernel folds them, with the sequence's own partial.
+#include <type_traits>
+
 #include "attn_unit.h"
 #include "prefix.h"
 
 namespace scout {
+
+typedef __attribute__((ext_vector_type(8))) short s16x8;
 
 // ---------------------------------------------------------------- the plan
 
@@ -376,6 +380,347 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(Pref
   }
 }
 
+// ---- More rows than that, bf16: tiles of K and V through LDS.
+//
+// A group of WM waves has WM * RW rows (each wave RW of them, in NT column tiles of 32) and takes WM units of 16 tokens at a time, a tile of
+// TOK = 16 * WM tokens: each wave brings one unit of K and V from memory into registers, and from there into LDS, where all of the group
+// read it.  WN groups take tiles in turn and fold their sums at the end.  Two tiles lie in LDS: while one is multiplied, the next one but one is on its
+// way from memory and the next one is stored.
+//   logits^T[token][row] = K . Q^T       32x32x16: K rows are the first operand (lane: token lane % 32, channels 8 * (lane / 32) + ..)
+//   out^T[channel][row] += V^T . P^T     32x32x16: the logits leave the first product with row lane % 32 and tokens 8 * (i / 4) + 4 * (lane / 32) +
+//                                        i % 4 in register i: eight registers are the second operand of a step of 16 tokens, if the
+//                                        first one, V^T, has its tokens in that order; the transposing LDS read delivers them
+// 16-byte chunk c of token row r lies at place c ^ swizzle(r) of its row, so that the lanes that LDS serves together hit different banks.
+// Units without a slot are left out: a window of 64 units is compacted before tiles are cut from it.
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+template <int DH>
+struct WideTile {
+  static constexpr int ROWB = DH * 2, CH = ROWB / 16;  // bytes and 16-byte chunks of a token row
+  static constexpr int NI = CH / 4;                    // 1 KiB pieces of a unit
+  static constexpr int KS = DH / 16, DT = DH / 32;     // steps of the first product, channel tiles of the second
+  static __device__ __forceinline__ int k_swizzle(int r) { return DH == 128 ? r & 15 : (r >> 1) & 7; }
+  static __device__ __forceinline__ int v_swizzle(int r) { return DH == 128 ? (r & 3) << 2 : (r & 2) << 1; }
+};
+
+// The units of an item that have a slot, in order, 64 at a time (lane j: the j-th).
+struct UnitWindow {
+  int slot, what;  // what: tokens that count (1 to 16; 0: no unit) | unit of the block << 8
+  int n, pos;      // units in the window, those that have been taken
+  int raw, raw_unit;  // the next window's entries as they are in the table (lane j: unit raw_unit + j)
+};
+
+template <int DH, int RW, int WM, int WN, int TERMS>
+__global__ __launch_bounds__(WM* WN* kWave) void prefix_wide_kernel(PrefixPlan P, PrefixStamp stamp, PrefixWork W) {
+  using L = WideTile<DH>;
+  constexpr int NT = RW / 32, TOK = 16 * WM, NH = TOK / 32, STEP = WM * WN;
+  constexpr int TILE = TOK * L::ROWB;  // bytes of K, and of V, of a tile
+  static_assert((WN - 1) * WM * (NT * L::DT * 16 + NT * 2) * 256 <= WN * 4 * TILE, "the groups' sums fit where the tiles were");
+  __shared__ __attribute__((aligned(1024))) char lds[WN * 4 * TILE];  // [group][buffer][K, V][tile]
+  if (!made_for(P, stamp) || (int)blockIdx.x >= P.head[0]) return;
+  const PrefixItem it = P.item[blockIdx.x];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int wm = wave % WM, grp = wave / WM, l32 = lane & 31, half = lane >> 5;
+  const int ush = W.s_shift - 4, u1 = (it.tok1 + kUnitTokens - 1) / kUnitTokens;
+  const int32_t* row = W.table + ((size_t)it.prefix * W.Hkv + it.head) * W.prefix_blocks;
+
+  UnitWindow U;
+  auto fetch_raw = [&](int unit) __attribute__((always_inline)) {
+    U.raw_unit = unit;
+    const int mine = unit + lane;
+    U.raw = mine < u1 ? row[mine >> ush] : -1;
+  };
+  // the next window with units in it, if there is one
+  auto next_window = [&]() __attribute__((always_inline)) {
+    U.pos = 0;
+    do {
+      const int unit = U.raw_unit + lane, left = it.tok1 - unit * kUnitTokens;
+      const bool ok = unit < u1 && U.raw >= 0 && U.raw < W.n_slots;
+      const uint64_t have = __ballot(ok);
+      int what = (left < kUnitTokens ? left : kUnitTokens) | (unit & ((1 << ush) - 1)) << 8;
+      // to the lane that is its rank among those that have a slot; the others' go to the last lane, which then has none
+      const int to = (ok ? mbcnt64(have) : kWave - 1) << 2;
+      U.n = (int)__popcll(have);
+      U.slot = __builtin_amdgcn_ds_permute(to, U.raw);
+      what = __builtin_amdgcn_ds_permute(to, what);
+      U.what = lane < U.n ? what : 0;
+      fetch_raw(U.raw_unit + kWave);
+    } while (U.n == 0 && U.raw_unit < u1);
+  };
+
+  fetch_raw(it.tok0 / kUnitTokens);
+  // the wave's rows as second operands of the first product: channels 16 * s + 8 * half on of row l32
+  bf16x8 q[NT][L::KS];
+  size_t out_row[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int r = wm * RW + t * 32 + l32;
+    const bool real = r < it.rows;
+    out_row[t] = query_row(P, W, it, real ? r : it.rows - 1);
+    const char* at = static_cast<const char*>(W.q) + out_row[t] * L::ROWB + half * 16;
+#pragma unroll
+    for (int s = 0; s < L::KS; ++s) {
+      u32x4 x = *reinterpret_cast<const u32x4*>(at + s * 32);
+      x &= real ? 0xffffffffu : 0u;
+      q[t][s] = as_bf16x8(x);
+    }
+  }
+
+  // Of the tile that a wave brings one unit of.
+  u32x4 stage_k[L::NI], stage_v[L::NI];
+  auto request = [&]() __attribute__((always_inline)) {  // the unit at U.pos + grp * WM + wm
+    const int j = U.pos + grp * WM + wm;
+    const int what = j < kWave ? __builtin_amdgcn_readlane(U.what, j & 63) : 0;
+    const long long slot = __builtin_amdgcn_readlane(U.slot, j & 63);
+    const int valid = what & 255;
+    const size_t off = valid > 0 ? ((size_t)slot * W.tile_stride + (size_t)(what >> 8) * kUnitTokens * DH) * 2 : 0;
+    const __amdgpu_buffer_rsrc_t kr =
+        __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(const_cast<void*>(W.k_pool)) + off, 0, valid * L::ROWB, 0x00020000);
+    const __amdgpu_buffer_rsrc_t vr =
+        __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(const_cast<void*>(W.v_pool)) + off, 0, valid * L::ROWB, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < L::NI; ++i)  // rows beyond the last token read as zeros
+      stage_k[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, i * 1024 + lane * 16, 0, 0));
+#pragma unroll
+    for (int i = 0; i < L::NI; ++i)
+      stage_v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, i * 1024 + lane * 16, 0, 0));
+  };
+  char* const mine = lds + grp * 4 * TILE;
+  auto store = [&](int buf) __attribute__((always_inline)) {
+    char* const k = mine + buf * 2 * TILE;
+#pragma unroll
+    for (int i = 0; i < L::NI; ++i) {
+      const int r = wm * 16 + i * (kWave / L::CH) + lane / L::CH, c = lane % L::CH;
+      *reinterpret_cast<u32x4*>(k + r * L::ROWB + (c ^ L::k_swizzle(r)) * 16) = stage_k[i];
+      *reinterpret_cast<u32x4*>(k + TILE + r * L::ROWB + (c ^ L::v_swizzle(r)) * 16) = stage_v[i];
+    }
+  };
+
+  f32x16 acc[NT][L::DT];
+  float m[NT], l[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+#pragma unroll
+    for (int d = 0; d < L::DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[t][d][i] = 0.0f;
+    m[t] = -INFINITY;
+    l[t] = 0.0f;
+  }
+
+  // What the wave reads of a tile: K chunk 2 * s + half of row l32, and the values of tokens 4 * half + lane % 16 / 4 on (16-byte chunk
+  // 4 * d + ..., 8 bytes of it).
+  const int k_at = l32 * L::ROWB, k_x = L::k_swizzle(l32);
+  const int v_tok = 4 * half + (lane & 15) / 4, v_x = L::v_swizzle(v_tok);
+  const int v_at = v_tok * L::ROWB + ((lane & 3) & 1) * 8, v_c = 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
+
+  // One tile of the group: `masked` if some of its tokens do not count; tokens[u] of unit u do.
+  auto compute = [&](int buf, auto masked, const int (&tokens)[WM]) __attribute__((always_inline)) {
+    const char* const k = mine + buf * 2 * TILE;
+    const char* const v = k + TILE;
+    f32x16 x[NT][NH];
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int hf = 0; hf < NH; ++hf)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[t][hf][i] = 0.0f;
+#pragma unroll
+    for (int hf = 0; hf < NH; ++hf)
+#pragma unroll
+      for (int s = 0; s < L::KS; ++s) {
+        const bf16x8 a = as_bf16x8(*reinterpret_cast<const u32x4*>(k + k_at + hf * 32 * L::ROWB + ((2 * s + half) ^ k_x) * 16));
+#pragma unroll
+        for (int t = 0; t < NT; ++t) x[t][hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[t][s], x[t][hf], 0, 0, 0);
+      }
+    s16x8 p[NT][TERMS][2 * NH];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      if constexpr (decltype(masked)::value) {
+#pragma unroll
+        for (int hf = 0; hf < NH; ++hf)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (8 * (i / 4 % 2) + 4 * half + i % 4 >= tokens[2 * hf + i / 8]) x[t][hf][i] = -INFINITY;
+      }
+      float bm = x[t][0][0];
+#pragma unroll
+      for (int hf = 0; hf < NH; ++hf)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) bm = fmaxf(bm, x[t][hf][i]);
+      bm = max_xor32(bm) * W.scale2;
+      const float m_new = fmaxf(m[t], bm), m_sub = m_new == -INFINITY ? 0.0f : m_new;
+      if (__ballot(m_new != m[t]) != 0) {
+        const float alpha = exp2_diff(m[t], m_new);
+        l[t] *= alpha;
+#pragma unroll
+        for (int d = 0; d < L::DT; ++d) acc[t][d] *= alpha;
+        m[t] = m_new;
+      }
+      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int hf = 0; hf < NH; ++hf)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {  // eight registers: a step of the second product
+          float w[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            w[e] = fast_exp2(fmaf(x[t][hf][8 * g + e], W.scale2, -m_sub));
+            sum[e & 3] += w[e];
+          }
+#pragma unroll
+          for (int n = 0; n < TERMS; ++n) {
+            u32x4 packed;
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+              if (n + 1 < TERMS) {  // cut, not rounded: what is left is not negative
+                const uint32_t a = __float_as_uint(w[e]), b = __float_as_uint(w[e + 1]);
+                packed[e / 2] = pack_halves(a, b, 1);
+                w[e] -= __uint_as_float(a & 0xffff0000u);
+                w[e + 1] -= __uint_as_float(b & 0xffff0000u);
+              } else if (TERMS > 1) {  // nothing left times an infinite value is not NaN
+                packed[e / 2] = cvt_pk_bf16(fmaxf(w[e], 0x1p-126f), fmaxf(w[e + 1], 0x1p-126f));
+              } else {
+                packed[e / 2] = cvt_pk_bf16(w[e], w[e + 1]);
+              }
+            }
+            p[t][n][2 * hf + g] = __builtin_bit_cast(s16x8, packed);
+          }
+        }
+      l[t] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    }
+#pragma unroll
+    for (int s = 0; s < 2 * NH; ++s)
+#pragma unroll
+      for (int d = 0; d < L::DT; ++d) {
+        typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+        const char* at = v + v_at + s * 16 * L::ROWB + ((4 * d + v_c) ^ v_x) * 16;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * L::ROWB));
+        const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int n = TERMS - 1; n >= 0; --n)
+            acc[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, p[t][n][s]), acc[t][d], 0, 0, 0);
+      }
+  };
+
+  next_window();
+  int buf = 0, tokens[WM];
+  bool more = U.n > 0;
+  auto look = [&]() __attribute__((always_inline)) {  // at the tokens of the group's tile at U.pos
+#pragma unroll
+    for (int u = 0; u < WM; ++u) {
+      const int j = U.pos + grp * WM + u;
+      tokens[u] = j < kWave ? __builtin_amdgcn_readlane(U.what, j & 63) & 255 : 0;
+    }
+  };
+  if (more) {
+    request();
+    int now[WM];
+    look();
+#pragma unroll
+    for (int u = 0; u < WM; ++u) now[u] = tokens[u];
+    auto advance = [&]() __attribute__((always_inline)) {
+      U.pos += STEP;
+      if (U.pos >= U.n) {
+        if (U.raw_unit < u1) next_window();
+        else U.n = 0;
+      }
+      return U.n > 0;
+    };
+    store(0);
+    more = advance();
+    if (more) {
+      request();
+      look();
+    }
+    __syncthreads();
+    while (true) {
+      int least = now[0], any = 0;
+#pragma unroll
+      for (int u = 0; u < WM; ++u) {
+        least = now[u] < least ? now[u] : least;
+        any |= now[u];
+      }
+      if (least == kUnitTokens) compute(buf, std::false_type{}, now);
+      else if (any) compute(buf, std::true_type{}, now);
+      if (!more) break;
+      buf ^= 1;
+      store(buf);
+#pragma unroll
+      for (int u = 0; u < WM; ++u) now[u] = tokens[u];
+      more = advance();
+      if (more) {
+        request();
+        look();
+      }
+      __syncthreads();
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) l[t] = sum_xor32(l[t]);
+
+  // the groups' sums, lane by lane, where the tiles were
+  if constexpr (WN > 1) {
+    constexpr int AREA = (NT * L::DT * 16 + NT * 2) * kWave;  // floats of a wave
+    float* const sums = reinterpret_cast<float*>(lds);
+    __syncthreads();
+    if (grp > 0) {
+      float* const to = sums + ((grp - 1) * WM + wm) * AREA + lane;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int d = 0; d < L::DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) to[((t * L::DT + d) * 16 + i) * kWave] = acc[t][d][i];
+        to[(NT * L::DT * 16 + 2 * t) * kWave] = m[t];
+        to[(NT * L::DT * 16 + 2 * t + 1) * kWave] = l[t];
+      }
+    }
+    __syncthreads();
+    if (grp > 0) return;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float M = m[t], f[WN];
+#pragma unroll
+      for (int g = 1; g < WN; ++g) M = fmaxf(M, sums[((g - 1) * WM + wm) * AREA + lane + (NT * L::DT * 16 + 2 * t) * kWave]);
+      f[0] = exp2_diff(m[t], M);
+      m[t] = M;
+      l[t] *= f[0];
+#pragma unroll
+      for (int d = 0; d < L::DT; ++d) acc[t][d] *= f[0];
+#pragma unroll
+      for (int g = 1; g < WN; ++g) {
+        const float* from = sums + ((g - 1) * WM + wm) * AREA + lane;
+        f[g] = exp2_diff(from[(NT * L::DT * 16 + 2 * t) * kWave], M);
+        l[t] += f[g] * from[(NT * L::DT * 16 + 2 * t + 1) * kWave];
+#pragma unroll
+        for (int d = 0; d < L::DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[t][d][i] += f[g] * from[((t * L::DT + d) * 16 + i) * kWave];
+      }
+    }
+  }
+  const int stride = P.head[1];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (wm * RW + t * 32 + l32 >= it.rows) continue;
+    const size_t at = out_row[t] * stride + it.split;
+#pragma unroll
+    for (int d = 0; d < L::DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<float4*>(W.po + at * DH + d * 32 + 8 * (i / 4) + 4 * half) =
+            make_float4(acc[t][d][i], acc[t][d][i + 1], acc[t][d][i + 2], acc[t][d][i + 3]);
+    if (half == 0) {
+      W.pm[at] = m[t];
+      W.pl[at] = l[t];
+    }
+  }
+}
+
 // ---------------------------------------------------------------- the splits, and the sequence's own partial
 
 struct PrefixOut {
@@ -467,9 +812,9 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(PrefixPlan P, Prefi
 // How the work of a batch is dealt: by the rows that a prefix has on average (the rows of a prefix with more are several tiles).
 static PrefixShape prefix_shape(const Dims& D, int dtype, int n_prefix) {
   const long long rows = ((long long)D.B * D.G + n_prefix - 1) / (n_prefix > 0 ? n_prefix : 1);
-  const int most = dtype == SCOUT_BF16 ? 64 : 32;  // fp32: twice the registers per row
   PrefixShape s;
-  s.tile_rows = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : 64;
+  if (dtype == SCOUT_F32) s.tile_rows = rows <= 16 ? 16 : 32;
+  else s.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   s.granule = 64;
   s.slots = 256;
   s.head_cost = 256;
@@ -502,20 +847,24 @@ int launch_prefix_plan(const Dims& D, int dtype, int n_prefix, int prefix_blocks
 }
 
 template <int DT, int DH, int TERMS>
-static void launch_narrow(int nq, int grid, const PrefixPlan& P, const PrefixStamp& stamp, const PrefixWork& W, hipStream_t st) {
-  const dim3 block(kNarrowWaves * kWave);
-  if (nq == 1) hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 1, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
-  else if (nq == 2 || DT == SCOUT_F32) hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 2, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
-  else if constexpr (DT == SCOUT_BF16)
-    hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 4, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
+static void launch_items(const PrefixShape& s, int grid, const PrefixPlan& P, const PrefixStamp& stamp, const PrefixWork& W, hipStream_t st) {
+  const dim3 block(512);
+  static_assert(kNarrowWaves * kWave == 512, "eight waves, whichever kernel");
+  if (s.tile_rows == 16) {
+    hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 1, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
+  } else if (s.tile_rows == 32) {
+    hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 2, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
+  } else if constexpr (DT == SCOUT_BF16) {
+    if (s.tile_rows == 64) hipLaunchKernelGGL((prefix_wide_kernel<DH, 32, 2, 4, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
+    else hipLaunchKernelGGL((prefix_wide_kernel<DH, 32, 4, 2, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
+  }
 }
 
 template <int DT, int DH>
 static void launch_all(const Dims& D, const PrefixShape& s, int items, const PrefixPlan& P, const PrefixStamp& stamp, const PrefixWork& W,
                        const PrefixOut& E, hipStream_t st) {
-  const int nq = s.tile_rows / 16;
-  if (DT == SCOUT_BF16 && E.o != nullptr) launch_narrow<DT, DH, 2>(nq, items, P, stamp, W, st);
-  else launch_narrow<DT, DH, 1>(nq, items, P, stamp, W, st);
+  if (DT == SCOUT_BF16 && E.o != nullptr) launch_items<DT, DH, 2>(s, items, P, stamp, W, st);
+  else launch_items<DT, DH, 1>(s, items, P, stamp, W, st);
   hipLaunchKernelGGL((prefix_combine_kernel<DT, DH>), dim3((D.B * D.Hq + 3) / 4), dim3(256), 0, st, P, stamp, W, E);
 }
 
