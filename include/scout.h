@@ -522,6 +522,8 @@ int scout_prefix_plan(const scout_problem* p, int32_t n_prefix, int32_t prefix_b
  *   out e [B][Hq][d], lse f32 [B][Hq]  out: the joined result as merge_partials writes
  *                 it; out may be NULL where o is given, lse always
  * A sequence without prefix and partial gives o = 0, m = -inf, l = 0, out = 0, lse = -inf.
+ * m is the reference that l and o are relative to: the largest logit, or up to 16 ln 2 below it
+ * (m + ln l is the same).
  * Products, sums and softmax weights are binary32; bf16 rounds the weights to bf16 before
  * the value product where only `out` is written, and to two bf16 terms (2^-16) where o is.
  */

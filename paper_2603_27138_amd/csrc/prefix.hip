@@ -179,8 +179,8 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(Pref
   using L = Tile<DT, DH>;
   constexpr int WAVES = kNarrowWaves, ROW = DH + 4;
   __shared__ float smem[WAVES * (16 * ROW + 32)];
+  const PrefixItem it = P.item[blockIdx.x];  // in the trip that says whether it is one
   if (!made_for(P, stamp) || (int)blockIdx.x >= P.head[0]) return;
-  const PrefixItem it = P.item[blockIdx.x];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), ln = lane & 15, kg = lane >> 4;
   const int ush = W.s_shift - 4;
   const int u0 = it.tok0 / kUnitTokens + wave, u1 = (it.tok1 + kUnitTokens - 1) / kUnitTokens;
@@ -382,131 +382,165 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(Pref
 
 // ---- More rows than that, bf16: tiles of K and V through LDS.
 //
-// A group of WM waves has WM * RW rows (each wave RW of them, in NT column tiles of 32) and takes WM units of 16 tokens at a time, a tile of
-// TOK = 16 * WM tokens: each wave brings one unit of K and V from memory into registers, and from there into LDS, where all of the group
-// read it.  WN groups take tiles in turn and fold their sums at the end.  Two tiles lie in LDS: while one is multiplied, the next one but one is on its
-// way from memory and the next one is stored.
+// A group of WM waves has WM * 32 rows (each wave 32 of them) and goes through tiles of TOK tokens, each wave bringing TOK / WM of their rows
+// from memory into LDS, where all of the group read them.  WN groups take tiles in turn and fold their sums at the end.  Two tiles
+// lie in LDS: while one is multiplied the next one is on its way, without passing through registers.
 //   logits^T[token][row] = K . Q^T       32x32x16: K rows are the first operand (lane: token lane % 32, channels 8 * (lane / 32) + ..)
 //   out^T[channel][row] += V^T . P^T     32x32x16: the logits leave the first product with row lane % 32 and tokens 8 * (i / 4) + 4 * (lane / 32) +
 //                                        i % 4 in register i: eight registers are the second operand of a step of 16 tokens, if the
 //                                        first one, V^T, has its tokens in that order; the transposing LDS read delivers them
 // 16-byte chunk c of token row r lies at place c ^ swizzle(r) of its row, so that the lanes that LDS serves together hit different banks.
-// Units without a slot are left out: a window of 64 units is compacted before tiles are cut from it.
+// Units of 16 tokens without a slot are left out: every tile but an item's last one is full.
 typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
 
 template <int DH>
 struct WideTile {
   static constexpr int ROWB = DH * 2, CH = ROWB / 16;  // bytes and 16-byte chunks of a token row
-  static constexpr int NI = CH / 4;                    // 1 KiB pieces of a unit
   static constexpr int KS = DH / 16, DT = DH / 32;     // steps of the first product, channel tiles of the second
   static __device__ __forceinline__ int k_swizzle(int r) { return DH == 128 ? r & 15 : (r >> 1) & 7; }
   static __device__ __forceinline__ int v_swizzle(int r) { return DH == 128 ? (r & 3) << 2 : (r & 2) << 1; }
 };
 
-// The units of an item that have a slot, in order, 64 at a time (lane j: the j-th).
-struct UnitWindow {
-  int slot, what;  // what: tokens that count (1 to 16; 0: no unit) | unit of the block << 8
-  int n, pos;      // units in the window, those that have been taken
-  int raw, raw_unit;  // the next window's entries as they are in the table (lane j: unit raw_unit + j)
-};
+// N pieces of 1 KiB, one after the other in memory from lane to lane in the order of at[], to LDS at `to`.  The compiler does not know of them:
+// await() says when they have arrived.
+template <int N>
+__device__ __forceinline__ void load_to_lds(const void* base, int bytes, const int (&at)[N], uint32_t to) {
+  const uint64_t b = reinterpret_cast<uint64_t>(base);
+  const i32x4 rsrc = {(int)(uint32_t)b, (int)(uint32_t)(b >> 32) & 0xffff, bytes, 0x00020000};
+  static_assert(N == 1 || N == 2 || N == 4, "pieces");
+  // a scalar write of m0 needs a wait state in front of the load that uses it
+  if constexpr (N == 1)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %0, 0 offen lds" ::"s"(rsrc), "s"(to), "v"(at[0]) : "memory");
+  else if constexpr (N == 2)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %0, 0 offen lds\n\t"
+                 "buffer_load_dwordx4 %3, %0, 0 offen offset:1024 lds" ::"s"(rsrc), "s"(to), "v"(at[0]), "v"(at[1])
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %0, 0 offen lds\n\t"
+                 "buffer_load_dwordx4 %3, %0, 0 offen offset:1024 lds\n\tbuffer_load_dwordx4 %4, %0, 0 offen offset:2048 lds\n\t"
+                 "buffer_load_dwordx4 %5, %0, 0 offen offset:3072 lds" ::"s"(rsrc), "s"(to), "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
+                 : "memory");
+}
+// All but the last N of the wave's loads from memory have arrived, and what it has read of LDS.
+template <int N>
+__device__ __forceinline__ void await() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
 
-template <int DH, int RW, int WM, int WN, int TERMS>
+// A row's sums are kept relative to a number that follows its maximum only when that has moved by more than 2^kLag: weights are below 2^kLag then,
+// which binary32 sums and bf16 terms hold as well as weights below one, and the sums need not be rescaled whenever one of a wave's
+// rows meets a larger logit, which is in most tiles.
+constexpr float kLag = 16.0f;
+
+template <int DH, int WM, int WN, int TOK, int TERMS>
 __global__ __launch_bounds__(WM* WN* kWave) void prefix_wide_kernel(PrefixPlan P, PrefixStamp stamp, PrefixWork W) {
   using L = WideTile<DH>;
-  constexpr int NT = RW / 32, TOK = 16 * WM, NH = TOK / 32, STEP = WM * WN;
-  constexpr int TILE = TOK * L::ROWB;  // bytes of K, and of V, of a tile
-  static_assert((WN - 1) * WM * (NT * L::DT * 16 + NT * 2) * 256 <= WN * 4 * TILE, "the groups' sums fit where the tiles were");
-  __shared__ __attribute__((aligned(1024))) char lds[WN * 4 * TILE];  // [group][buffer][K, V][tile]
+  constexpr int NH = TOK / 32, UNITS = TOK / 16, STEP = UNITS * WN;
+  constexpr int TILE = TOK * L::ROWB;                // bytes of K, and of V, of a tile
+  constexpr int MINE = TILE / WM, NP = MINE / 1024;  // bytes and pieces of it that a wave brings
+  constexpr int ROWS = TOK / WM;                     // token rows of it
+  typedef std::conditional_t<(UNITS > 4), uint64_t, uint32_t> Counts;  // tokens that count of each unit of a tile, a byte for each
+  static_assert(UNITS <= 8 && ROWS <= 16 && MINE % 1024 == 0, "a wave's rows are of one unit, in whole pieces");
+  static_assert(STEP <= 32, "steps are cut from 64 units");
+  static_assert((WN - 1) * WM * (L::DT * 16 + 2) * 256 <= WN * 4 * TILE, "the groups' sums fit where the tiles were");
+  __shared__ __attribute__((aligned(1024))) char lds[WN * 4 * TILE];  // [group][tile at hand or next][K, V][tile]
+  __shared__ int2 queue[WM * WN][kWave];
+  const PrefixItem it = P.item[blockIdx.x];  // in the trip that says whether it is one
   if (!made_for(P, stamp) || (int)blockIdx.x >= P.head[0]) return;
-  const PrefixItem it = P.item[blockIdx.x];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wm = wave % WM, grp = wave / WM, l32 = lane & 31, half = lane >> 5;
   const int ush = W.s_shift - 4, u1 = (it.tok1 + kUnitTokens - 1) / kUnitTokens;
   const int32_t* row = W.table + ((size_t)it.prefix * W.Hkv + it.head) * W.prefix_blocks;
 
-  UnitWindow U;
-  auto fetch_raw = [&](int unit) __attribute__((always_inline)) {
-    U.raw_unit = unit;
+  // The item's units that have a slot, in order, up to 64 at a time: lane j has the j-th's slot, and its tokens that count (16, or fewer
+  // in the prefix's last unit; 0: no unit) | unit of the block << 8.  Behind them the table's entries that are still to be looked through
+  // (of units raw_unit on, a bit of `pending` for each that has a slot), and those that are on their way.
+  int u_slot = 0, u_what = 0, u_n = 0, u_pos = 0;
+  uint64_t u_full = 0;
+  int raw = 0, raw_what = 0, ahead, ahead_unit;
+  uint64_t pending = 0;
+  auto fetch = [&](int unit) __attribute__((always_inline)) {
+    ahead_unit = unit;
     const int mine = unit + lane;
-    U.raw = mine < u1 ? row[mine >> ush] : -1;
+    ahead = mine < u1 ? row[mine >> ush] : -1;
   };
-  // the next window with units in it, if there is one
-  auto next_window = [&]() __attribute__((always_inline)) {
-    U.pos = 0;
-    do {
-      const int unit = U.raw_unit + lane, left = it.tok1 - unit * kUnitTokens;
-      const bool ok = unit < u1 && U.raw >= 0 && U.raw < W.n_slots;
-      const uint64_t have = __ballot(ok);
-      int what = (left < kUnitTokens ? left : kUnitTokens) | (unit & ((1 << ush) - 1)) << 8;
-      // to the lane that is its rank among those that have a slot; the others' go to the last lane, which then has none
-      const int to = (ok ? mbcnt64(have) : kWave - 1) << 2;
-      U.n = (int)__popcll(have);
-      U.slot = __builtin_amdgcn_ds_permute(to, U.raw);
-      what = __builtin_amdgcn_ds_permute(to, what);
-      U.what = lane < U.n ? what : 0;
-      fetch_raw(U.raw_unit + kWave);
-    } while (U.n == 0 && U.raw_unit < u1);
+  // A step's units at least, as long as there are any: what is left moves to the front, what comes next joins it.
+  auto refill = [&]() __attribute__((always_inline)) {
+    int2* const q = queue[wave];
+    int n = u_n - u_pos;
+    if (lane >= u_pos && lane < u_n) q[lane - u_pos] = make_int2(u_slot, u_what);
+    while (n < kWave && (pending != 0 || ahead_unit < u1)) {
+      if (pending == 0) {
+        const int unit = ahead_unit + lane, left = it.tok1 - unit * kUnitTokens;
+        raw = ahead;
+        raw_what = (left < kUnitTokens ? left : kUnitTokens) | (unit & ((1 << ush) - 1)) << 8;
+        pending = __ballot(unit < u1 && raw >= 0 && raw < W.n_slots);
+        fetch(ahead_unit + kWave);
+      }
+      const int rank = mbcnt64(pending);
+      const bool takes = (pending >> lane & 1) != 0 && rank < kWave - n;
+      if (takes) q[n + rank] = make_int2(raw, raw_what);
+      const uint64_t taken = __ballot(takes);
+      pending &= ~taken;
+      n += (int)__popcll(taken);
+    }
+    u_pos = 0;
+    u_n = n;
+    const int2 mine = q[lane];
+    u_slot = mine.x;
+    u_what = lane < n ? mine.y : 0;
+    u_full = __ballot((u_what & 255) == kUnitTokens);
   };
 
-  fetch_raw(it.tok0 / kUnitTokens);
+  fetch(it.tok0 / kUnitTokens);
   // the wave's rows as second operands of the first product: channels 16 * s + 8 * half on of row l32
-  bf16x8 q[NT][L::KS];
-  size_t out_row[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int r = wm * RW + t * 32 + l32;
-    const bool real = r < it.rows;
-    out_row[t] = query_row(P, W, it, real ? r : it.rows - 1);
-    const char* at = static_cast<const char*>(W.q) + out_row[t] * L::ROWB + half * 16;
+  bf16x8 q[L::KS];
+  const bool real = wm * 32 + l32 < it.rows;
+  const size_t out_row = query_row(P, W, it, real ? wm * 32 + l32 : it.rows - 1);
+  {
+    const char* at = static_cast<const char*>(W.q) + out_row * L::ROWB + half * 16;
 #pragma unroll
     for (int s = 0; s < L::KS; ++s) {
-      u32x4 x = *reinterpret_cast<const u32x4*>(at + s * 32);
-      x &= real ? 0xffffffffu : 0u;
-      q[t][s] = as_bf16x8(x);
+      u32x4 y = *reinterpret_cast<const u32x4*>(at + s * 32);
+      y &= real ? 0xffffffffu : 0u;
+      q[s] = as_bf16x8(y);
     }
   }
 
-  // Of the tile that a wave brings one unit of.
-  u32x4 stage_k[L::NI], stage_v[L::NI];
-  auto request = [&]() __attribute__((always_inline)) {  // the unit at U.pos + grp * WM + wm
-    const int j = U.pos + grp * WM + wm;
-    const int what = j < kWave ? __builtin_amdgcn_readlane(U.what, j & 63) : 0;
-    const long long slot = __builtin_amdgcn_readlane(U.slot, j & 63);
-    const int valid = what & 255;
-    const size_t off = valid > 0 ? ((size_t)slot * W.tile_stride + (size_t)(what >> 8) * kUnitTokens * DH) * 2 : 0;
-    const __amdgpu_buffer_rsrc_t kr =
-        __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(const_cast<void*>(W.k_pool)) + off, 0, valid * L::ROWB, 0x00020000);
-    const __amdgpu_buffer_rsrc_t vr =
-        __builtin_amdgcn_make_buffer_rsrc(static_cast<char*>(const_cast<void*>(W.v_pool)) + off, 0, valid * L::ROWB, 0x00020000);
+  // Where a lane's 16 bytes of the wave's pieces lie in memory, from the first of its rows on: place lane % CH of row r holds chunk
+  // place ^ swizzle(r); less the kibibytes that the loads add to both addresses.
+  int k_from[NP], v_from[NP];
+  const int row0 = wm * ROWS;
 #pragma unroll
-    for (int i = 0; i < L::NI; ++i)  // rows beyond the last token read as zeros
-      stage_k[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, i * 1024 + lane * 16, 0, 0));
-#pragma unroll
-    for (int i = 0; i < L::NI; ++i)
-      stage_v[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, i * 1024 + lane * 16, 0, 0));
-  };
+  for (int i = 0; i < NP; ++i) {
+    const int in = lane / L::CH, r = row0 + i * (kWave / L::CH) + in, c = lane % L::CH;
+    k_from[i] = in * L::ROWB + ((c ^ L::k_swizzle(r)) << 4);
+    v_from[i] = in * L::ROWB + ((c ^ L::v_swizzle(r)) << 4);
+  }
+  typedef __attribute__((address_space(3))) char* lds_ptr;
   char* const mine = lds + grp * 4 * TILE;
-  auto store = [&](int buf) __attribute__((always_inline)) {
-    char* const k = mine + buf * 2 * TILE;
-#pragma unroll
-    for (int i = 0; i < L::NI; ++i) {
-      const int r = wm * 16 + i * (kWave / L::CH) + lane / L::CH, c = lane % L::CH;
-      *reinterpret_cast<u32x4*>(k + r * L::ROWB + (c ^ L::k_swizzle(r)) * 16) = stage_k[i];
-      *reinterpret_cast<u32x4*>(k + TILE + r * L::ROWB + (c ^ L::v_swizzle(r)) * 16) = stage_v[i];
-    }
+  const uint32_t lds_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)mine + wm * MINE);
+  // The wave's part of the group's tile at u_pos, to place `to` (0 or 1).
+  auto request = [&](int to) __attribute__((always_inline)) {
+    const int j = u_pos + grp * UNITS + row0 / 16;
+    const int what = j < kWave ? __builtin_amdgcn_readlane(u_what, j & 63) : 0;
+    const long long slot = __builtin_amdgcn_readlane(u_slot, j & 63);
+    const int valid = (what & 255) - row0 % 16;
+    const size_t off = valid > 0 ? ((size_t)slot * W.tile_stride + (size_t)((what >> 8) * kUnitTokens + row0 % 16) * DH) * 2 : 0;
+    const int bytes = valid > 0 ? valid * L::ROWB : 0;
+    load_to_lds<NP>(static_cast<const char*>(W.k_pool) + off, bytes, k_from, lds_at + to * 2 * TILE);
+    load_to_lds<NP>(static_cast<const char*>(W.v_pool) + off, bytes, v_from, lds_at + to * 2 * TILE + TILE);
   };
+  constexpr uint64_t STEP_BITS = (1ull << STEP) - 1;
+  auto is_full = [&]() __attribute__((always_inline)) { return (u_full >> u_pos & STEP_BITS) == STEP_BITS; };
 
-  f32x16 acc[NT][L::DT];
-  float m[NT], l[NT];
+  f32x16 acc[L::DT];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
+  for (int d = 0; d < L::DT; ++d)
 #pragma unroll
-    for (int d = 0; d < L::DT; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[t][d][i] = 0.0f;
-    m[t] = -INFINITY;
-    l[t] = 0.0f;
-  }
+    for (int i = 0; i < 16; ++i) acc[d][i] = 0.0f;
+  float m = -INFINITY, l = 0.0f;
 
   // What the wave reads of a tile: K chunk 2 * s + half of row l32, and the values of tokens 4 * half + lane % 16 / 4 on (16-byte chunk
   // 4 * d + ..., 8 bytes of it).
@@ -514,210 +548,194 @@ __global__ __launch_bounds__(WM* WN* kWave) void prefix_wide_kernel(PrefixPlan P
   const int v_tok = 4 * half + (lane & 15) / 4, v_x = L::v_swizzle(v_tok);
   const int v_at = v_tok * L::ROWB + ((lane & 3) & 1) * 8, v_c = 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
 
-  // One tile of the group: `masked` if some of its tokens do not count; tokens[u] of unit u do.
-  auto compute = [&](int buf, auto masked, const int (&tokens)[WM]) __attribute__((always_inline)) {
-    const char* const k = mine + buf * 2 * TILE;
-    const char* const v = k + TILE;
-    f32x16 x[NT][NH];
+  f32x16 x[NH];
+  auto logits = [&](const char* k) __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int hf = 0; hf < NH; ++hf)
 #pragma unroll
-      for (int hf = 0; hf < NH; ++hf)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[t][hf][i] = 0.0f;
+      for (int i = 0; i < 16; ++i) x[hf][i] = 0.0f;
 #pragma unroll
     for (int hf = 0; hf < NH; ++hf)
 #pragma unroll
       for (int s = 0; s < L::KS; ++s) {
         const bf16x8 a = as_bf16x8(*reinterpret_cast<const u32x4*>(k + k_at + hf * 32 * L::ROWB + ((2 * s + half) ^ k_x) * 16));
-#pragma unroll
-        for (int t = 0; t < NT; ++t) x[t][hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[t][s], x[t][hf], 0, 0, 0);
+        x[hf] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[s], x[hf], 0, 0, 0);
       }
-    s16x8 p[NT][TERMS][2 * NH];
+  };
+  auto largest = [&]() __attribute__((always_inline)) {  // of the tile's logits, in base-2 units
+    float b = x[0][0];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      if constexpr (decltype(masked)::value) {
+    for (int hf = 0; hf < NH; ++hf)
 #pragma unroll
-        for (int hf = 0; hf < NH; ++hf)
+      for (int i = 0; i < 16; ++i) b = fmaxf(b, x[hf][i]);
+    return max_xor32(b) * W.scale2;
+  };
+  auto follow = [&](float b) __attribute__((always_inline)) {  // the maximum, where it has moved far
+    const float m_new = b > m + kLag ? b : m, alpha = exp2_diff(m, m_new);
+    l *= alpha;
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (8 * (i / 4 % 2) + 4 * half + i % 4 >= tokens[2 * hf + i / 8]) x[t][hf][i] = -INFINITY;
+    for (int d = 0; d < L::DT; ++d) acc[d] *= alpha;
+    m = m_new;
+  };
+  auto values = [&](const char* v) __attribute__((always_inline)) {  // the logits' weights, and the weighted values
+    const float m_sub = m == -INFINITY ? 0.0f : m;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    s16x8 p[TERMS][UNITS];
+#pragma unroll
+    for (int s = 0; s < UNITS; ++s) {  // eight registers: a step of the second product
+      float w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        w[e] = fast_exp2(fmaf(x[s / 2][8 * (s % 2) + e], W.scale2, -m_sub));
+        sum[e & 3] += w[e];
       }
-      float bm = x[t][0][0];
 #pragma unroll
-      for (int hf = 0; hf < NH; ++hf)
+      for (int n = 0; n < TERMS; ++n) {
+        u32x4 packed;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) bm = fmaxf(bm, x[t][hf][i]);
-      bm = max_xor32(bm) * W.scale2;
-      const float m_new = fmaxf(m[t], bm), m_sub = m_new == -INFINITY ? 0.0f : m_new;
-      if (__ballot(m_new != m[t]) != 0) {
-        const float alpha = exp2_diff(m[t], m_new);
-        l[t] *= alpha;
-#pragma unroll
-        for (int d = 0; d < L::DT; ++d) acc[t][d] *= alpha;
-        m[t] = m_new;
-      }
-      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int hf = 0; hf < NH; ++hf)
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {  // eight registers: a step of the second product
-          float w[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            w[e] = fast_exp2(fmaf(x[t][hf][8 * g + e], W.scale2, -m_sub));
-            sum[e & 3] += w[e];
-          }
-#pragma unroll
-          for (int n = 0; n < TERMS; ++n) {
-            u32x4 packed;
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-              if (n + 1 < TERMS) {  // cut, not rounded: what is left is not negative
-                const uint32_t a = __float_as_uint(w[e]), b = __float_as_uint(w[e + 1]);
-                packed[e / 2] = pack_halves(a, b, 1);
-                w[e] -= __uint_as_float(a & 0xffff0000u);
-                w[e + 1] -= __uint_as_float(b & 0xffff0000u);
-              } else if (TERMS > 1) {  // nothing left times an infinite value is not NaN
-                packed[e / 2] = cvt_pk_bf16(fmaxf(w[e], 0x1p-126f), fmaxf(w[e + 1], 0x1p-126f));
-              } else {
-                packed[e / 2] = cvt_pk_bf16(w[e], w[e + 1]);
-              }
-            }
-            p[t][n][2 * hf + g] = __builtin_bit_cast(s16x8, packed);
+        for (int e = 0; e < 8; e += 2) {
+          if (n + 1 < TERMS) {  // cut, not rounded: what is left is not negative
+            const uint32_t a = __float_as_uint(w[e]), b = __float_as_uint(w[e + 1]);
+            packed[e / 2] = pack_halves(a, b, 1);
+            w[e] -= __uint_as_float(a & 0xffff0000u);
+            w[e + 1] -= __uint_as_float(b & 0xffff0000u);
+          } else if (TERMS > 1) {  // nothing left times an infinite value is not NaN
+            packed[e / 2] = cvt_pk_bf16(fmaxf(w[e], 0x1p-126f), fmaxf(w[e + 1], 0x1p-126f));
+          } else {
+            packed[e / 2] = cvt_pk_bf16(w[e], w[e + 1]);
           }
         }
-      l[t] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        p[n][s] = __builtin_bit_cast(s16x8, packed);
+      }
     }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
-    for (int s = 0; s < 2 * NH; ++s)
+    for (int s = 0; s < UNITS; ++s)
 #pragma unroll
       for (int d = 0; d < L::DT; ++d) {
-        typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+        typedef __attribute__((address_space(3))) s16x4* tr_ptr;
         const char* at = v + v_at + s * 16 * L::ROWB + ((4 * d + v_c) ^ v_x) * 16;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 8 * L::ROWB));
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(at));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((tr_ptr)(at + 8 * L::ROWB));
         const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int n = TERMS - 1; n >= 0; --n)
-            acc[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, p[t][n][s]), acc[t][d], 0, 0, 0);
+        for (int n = TERMS - 1; n >= 0; --n)
+          acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, p[n][s]), acc[d], 0, 0, 0);
       }
   };
 
-  next_window();
-  int buf = 0, tokens[WM];
-  bool more = U.n > 0;
-  auto look = [&]() __attribute__((always_inline)) {  // at the tokens of the group's tile at U.pos
-#pragma unroll
-    for (int u = 0; u < WM; ++u) {
-      const int j = U.pos + grp * WM + u;
-      tokens[u] = j < kWave ? __builtin_amdgcn_readlane(U.what, j & 63) & 255 : 0;
-    }
+  // The wave's part of the tile has arrived, so has everybody's behind the barrier, and nobody reads the tile before it any more.
+  auto arrive = [&]() __attribute__((always_inline)) {
+    await<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   };
-  if (more) {
-    request();
-    int now[WM];
-    look();
+  refill();
+  if (u_n > 0) {
+    int at = 0;
+    bool full = is_full(), more;  // the step at hand is full; another one follows
+    Counts tokens = 0;            // of the group's tile in the step at hand, where that is not full
+    auto count = [&]() __attribute__((always_inline)) {
+      tokens = 0;
 #pragma unroll
-    for (int u = 0; u < WM; ++u) now[u] = tokens[u];
-    auto advance = [&]() __attribute__((always_inline)) {
-      U.pos += STEP;
-      if (U.pos >= U.n) {
-        if (U.raw_unit < u1) next_window();
-        else U.n = 0;
+      for (int u = 0; u < UNITS; ++u) {
+        const int j = u_pos + grp * UNITS + u;
+        tokens |= (Counts)(j < kWave ? __builtin_amdgcn_readlane(u_what, j & 63) & 255 : 0) << (8 * u);
       }
-      return U.n > 0;
     };
-    store(0);
-    more = advance();
-    if (more) {
-      request();
-      look();
+    // The step at u_pos is on its way to place `at`; ask for the one behind it.
+    auto go_on = [&]() __attribute__((always_inline)) {
+      full = is_full();
+      if (!full) count();
+      u_pos += STEP;
+      if (u_n - u_pos < STEP) refill();
+      more = u_n > u_pos;
+    };
+    request(0);
+    go_on();
+    arrive();
+    if (more) request(1);
+    // full tiles: the branch to follow() is rare, and left out of the loop, where it would cost every tile copies of the sums
+    while (full) {
+      logits(mine + at * 2 * TILE);
+      float b = largest();
+      if (__ballot(b > m + kLag) != 0) follow(b);
+      values(mine + at * 2 * TILE + TILE);
+      if (!more) {
+        full = false;
+        tokens = 0;
+        break;
+      }
+      at ^= 1;
+      go_on();
+      arrive();
+      if (more) request(at ^ 1);
     }
-    __syncthreads();
-    while (true) {
-      int least = now[0], any = 0;
+    if (tokens != 0) {  // the last step's tile is not full
+      char* const v = mine + at * 2 * TILE + TILE;
+      logits(mine + at * 2 * TILE);
 #pragma unroll
-      for (int u = 0; u < WM; ++u) {
-        least = now[u] < least ? now[u] : least;
-        any |= now[u];
-      }
-      if (least == kUnitTokens) compute(buf, std::false_type{}, now);
-      else if (any) compute(buf, std::true_type{}, now);
-      if (!more) break;
-      buf ^= 1;
-      store(buf);
+      for (int hf = 0; hf < NH; ++hf)
 #pragma unroll
-      for (int u = 0; u < WM; ++u) now[u] = tokens[u];
-      more = advance();
-      if (more) {
-        request();
-        look();
+        for (int i = 0; i < 16; ++i)
+          if (8 * (i / 4 % 2) + 4 * half + i % 4 >= (int)(tokens >> (8 * (2 * hf + i / 8)) & 255)) x[hf][i] = -INFINITY;
+      // rows that do not count become zero, whatever lies there (every wave sees to that by itself: LDS serves a wave's accesses in order)
+      for (int c = lane; c < TOK * L::CH; c += kWave) {
+        const int r = c / L::CH;
+        if (r % 16 >= (int)(tokens >> (8 * (r / 16)) & 255)) *reinterpret_cast<u32x4*>(v + c * 16) = (u32x4){0, 0, 0, 0};
       }
-      __syncthreads();
+      follow(largest());
+      values(v);
     }
   }
-#pragma unroll
-  for (int t = 0; t < NT; ++t) l[t] = sum_xor32(l[t]);
+  l = sum_xor32(l);
 
   // the groups' sums, lane by lane, where the tiles were
   if constexpr (WN > 1) {
-    constexpr int AREA = (NT * L::DT * 16 + NT * 2) * kWave;  // floats of a wave
+    constexpr int AREA = (L::DT * 16 + 2) * kWave;  // floats of a wave
     float* const sums = reinterpret_cast<float*>(lds);
     __syncthreads();
     if (grp > 0) {
       float* const to = sums + ((grp - 1) * WM + wm) * AREA + lane;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
+      for (int d = 0; d < L::DT; ++d)
 #pragma unroll
-        for (int d = 0; d < L::DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) to[((t * L::DT + d) * 16 + i) * kWave] = acc[t][d][i];
-        to[(NT * L::DT * 16 + 2 * t) * kWave] = m[t];
-        to[(NT * L::DT * 16 + 2 * t + 1) * kWave] = l[t];
-      }
+        for (int i = 0; i < 16; ++i) to[(d * 16 + i) * kWave] = acc[d][i];
+      to[L::DT * 16 * kWave] = m;
+      to[(L::DT * 16 + 1) * kWave] = l;
     }
     __syncthreads();
     if (grp > 0) return;
+    float M = m;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      float M = m[t], f[WN];
+    for (int g = 1; g < WN; ++g) M = fmaxf(M, sums[((g - 1) * WM + wm) * AREA + lane + L::DT * 16 * kWave]);
+    const float f0 = exp2_diff(m, M);
+    m = M;
+    l *= f0;
 #pragma unroll
-      for (int g = 1; g < WN; ++g) M = fmaxf(M, sums[((g - 1) * WM + wm) * AREA + lane + (NT * L::DT * 16 + 2 * t) * kWave]);
-      f[0] = exp2_diff(m[t], M);
-      m[t] = M;
-      l[t] *= f[0];
+    for (int d = 0; d < L::DT; ++d) acc[d] *= f0;
 #pragma unroll
-      for (int d = 0; d < L::DT; ++d) acc[t][d] *= f[0];
+    for (int g = 1; g < WN; ++g) {
+      const float* from = sums + ((g - 1) * WM + wm) * AREA + lane;
+      const float f = exp2_diff(from[L::DT * 16 * kWave], M);
+      l += f * from[(L::DT * 16 + 1) * kWave];
 #pragma unroll
-      for (int g = 1; g < WN; ++g) {
-        const float* from = sums + ((g - 1) * WM + wm) * AREA + lane;
-        f[g] = exp2_diff(from[(NT * L::DT * 16 + 2 * t) * kWave], M);
-        l[t] += f[g] * from[(NT * L::DT * 16 + 2 * t + 1) * kWave];
+      for (int d = 0; d < L::DT; ++d)
 #pragma unroll
-        for (int d = 0; d < L::DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[t][d][i] += f[g] * from[((t * L::DT + d) * 16 + i) * kWave];
-      }
+        for (int i = 0; i < 16; ++i) acc[d][i] += f * from[(d * 16 + i) * kWave];
     }
   }
-  const int stride = P.head[1];
+  if (!real) return;
+  const size_t to = out_row * P.head[1] + it.split;
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    if (wm * RW + t * 32 + l32 >= it.rows) continue;
-    const size_t at = out_row[t] * stride + it.split;
+  for (int d = 0; d < L::DT; ++d)
 #pragma unroll
-    for (int d = 0; d < L::DT; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<float4*>(W.po + at * DH + d * 32 + 8 * (i / 4) + 4 * half) =
-            make_float4(acc[t][d][i], acc[t][d][i + 1], acc[t][d][i + 2], acc[t][d][i + 3]);
-    if (half == 0) {
-      W.pm[at] = m[t];
-      W.pl[at] = l[t];
-    }
+    for (int i = 0; i < 16; i += 4)
+      *reinterpret_cast<float4*>(W.po + to * DH + d * 32 + 8 * (i / 4) + 4 * half) =
+          make_float4(acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]);
+  if (half == 0) {
+    W.pm[to] = m;
+    W.pl[to] = l;
   }
 }
 
@@ -761,17 +779,21 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(PrefixPlan P, Prefi
 #pragma unroll
   for (int s = 1; s < kWave; s <<= 1) ls += __shfl_xor(ls, s);
   chans o{};
-  for (int s0 = 0; s0 < n; s0 += 4) {
-    chans x[4];
+  constexpr int TRIP = 16;  // splits requested at a time
+  const __amdgpu_buffer_rsrc_t sums = __builtin_amdgcn_make_buffer_rsrc(W.po + at * DH, 0, n * DH * 4, 0x00020000);  // beyond: zeros
+  for (int s0 = 0; s0 < n; s0 += TRIP) {
+    chans x[TRIP];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      x[u] = *reinterpret_cast<const chans*>(W.po + (at + (s0 + u < n ? s0 + u : n - 1)) * DH + c);
+    for (int u = 0; u < TRIP; ++u) {
+      const int off = ((s0 + u) * DH + c) * 4;
+      if constexpr (N == 2) x[u] = __builtin_bit_cast(chans, __builtin_amdgcn_raw_buffer_load_b64(sums, off, 0, 0));
+      else x[u][0] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sums, off, 0, 0));
+    }
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (s0 + u < n) {
-        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s0 + u));
-        if (w > 0.0f) o += w * x[u];  // a split without tokens has no weight
-      }
+    for (int u = 0; u < TRIP; ++u) {
+      const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s0 + u));
+      if (w != 0.0f) o += w * x[u];  // a split without tokens has no weight
+    }
   }
   // The two partials as one.  A side without tokens (sum zero) has no weight, whatever its other numbers; a sum that is NaN
   // stays one.
@@ -814,7 +836,7 @@ static PrefixShape prefix_shape(const Dims& D, int dtype, int n_prefix) {
   const long long rows = ((long long)D.B * D.G + n_prefix - 1) / (n_prefix > 0 ? n_prefix : 1);
   PrefixShape s;
   if (dtype == SCOUT_F32) s.tile_rows = rows <= 16 ? 16 : 32;
-  else s.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  else s.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
   s.granule = 64;
   s.slots = 256;
   s.head_cost = 256;
@@ -848,15 +870,15 @@ int launch_prefix_plan(const Dims& D, int dtype, int n_prefix, int prefix_blocks
 
 template <int DT, int DH, int TERMS>
 static void launch_items(const PrefixShape& s, int grid, const PrefixPlan& P, const PrefixStamp& stamp, const PrefixWork& W, hipStream_t st) {
-  const dim3 block(512);
-  static_assert(kNarrowWaves * kWave == 512, "eight waves, whichever kernel");
+  const dim3 g(grid);
   if (s.tile_rows == 16) {
-    hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 1, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
+    hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 1, TERMS>), g, dim3(512), 0, st, P, stamp, W);
   } else if (s.tile_rows == 32) {
-    hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 2, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
+    hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 2, TERMS>), g, dim3(512), 0, st, P, stamp, W);
   } else if constexpr (DT == SCOUT_BF16) {
-    if (s.tile_rows == 64) hipLaunchKernelGGL((prefix_wide_kernel<DH, 32, 2, 4, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
-    else hipLaunchKernelGGL((prefix_wide_kernel<DH, 32, 4, 2, TERMS>), dim3(grid), block, 0, st, P, stamp, W);
+    if (s.tile_rows == 64) hipLaunchKernelGGL((prefix_wide_kernel<DH, 2, 4, 32, TERMS>), g, dim3(512), 0, st, P, stamp, W);
+    else if (s.tile_rows == 128) hipLaunchKernelGGL((prefix_wide_kernel<DH, 4, 2, 64, TERMS>), g, dim3(512), 0, st, P, stamp, W);
+    else hipLaunchKernelGGL((prefix_wide_kernel<DH, 8, 1, 128, TERMS>), g, dim3(512), 0, st, P, stamp, W);
   }
 }
 
