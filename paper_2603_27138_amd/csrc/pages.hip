@@ -7,8 +7,8 @@
 // head, block), by ranks: the r-th taker gets the r-th clear bit.  So the same state gives the same slots, whatever order
 // the workgroups run in; the atomics that count references up and down are integer additions, whose order changes nothing.
 //
-// A fork and a compaction are two launches: one workgroup that plans (who is refused, which ranks, which slots), and a launch
-// that moves bytes (digest rows, table rows, tiles).
+// A fork and a compaction plan in one launch (who is refused, which ranks, which slots) and move bytes in the next one (digest rows,
+// table rows, tiles).
 #include "pages.h"
 
 namespace scout {
@@ -84,6 +84,7 @@ __device__ __forceinline__ bool has_slot(int entry, long long n_slots) { return 
 __global__ __launch_bounds__(kCopyThreads) void pages_clear_kernel(Pages P) {
   const long long n = P.n_slots, step = (long long)gridDim.x * kCopyThreads;
   for (long long i = (long long)blockIdx.x * kCopyThreads + threadIdx.x; i < n; i += step) P.refs[i] = 0;
+  for (long long i = (long long)blockIdx.x * kCopyThreads + threadIdx.x; i < Pages::kPairs; i += step) P.arrived[i] = 0;
 }
 
 __global__ __launch_bounds__(kCopyThreads) void pages_count_kernel(Dims D, Pages P, const int32_t* __restrict__ ctx_len,
@@ -141,101 +142,152 @@ __device__ __forceinline__ bool is_copied(const Dims& D, bool deep, int ctx, int
   return deep ? j < nb : j == nb - 1 && (ctx & (D.S - 1)) != 0 && ctx < D.max_blocks * D.S;
 }
 
-// Which forks are refused, the ranks of the slots that the others need, and these slots.
+// Entries with a slot of every row that a deep fork copies: a workgroup per row.
+__global__ __launch_bounds__(kCopyThreads) void fork_count_kernel(Dims D, Pages P, const int32_t* __restrict__ src,
+                                                                  const int32_t* __restrict__ ctx_len, const int32_t* __restrict__ table) {
+  __shared__ int lds[kCopyThreads / kWave];
+  const int r = blockIdx.x, i = r / D.Hkv, s = src[i];
+  int c = 0;
+  if (s >= 0 && s < D.B) {
+    const int nb = num_blocks(D, ctx_len[s]);
+    const int32_t* row = table + ((size_t)s * D.Hkv + (r - i * D.Hkv)) * D.max_blocks;
+#pragma unroll 4
+    for (int j = threadIdx.x; j < nb; j += kCopyThreads) c += has_slot(row[j], P.n_slots);
+  }
+  c = wave_scan(c, lane_id());
+  if (lane_id() == kWave - 1) lds[threadIdx.x / kWave] = c;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < kCopyThreads / kWave; ++w) all += lds[w];
+    P.base[r] = all;
+  }
+}
+
+// Which forks are refused, the ranks of the slots that the others need (of a deep fork: from the counts in P.base), and these slots.
 __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(Dims D, Pages P, int n, const int32_t* __restrict__ src,
                                                                  const int32_t* __restrict__ dst, int deep,
                                                                  const int32_t* __restrict__ ctx_len,
                                                                  const int32_t* __restrict__ table, int32_t* status) {
   __shared__ int lds[kPlanWaves];
-  const int lane = lane_id(), wave = threadIdx.x / kWave;
-  for (int i = threadIdx.x; i < n; i += kPlanThreads) {
-    const int s = src[i], t = dst[i];
+  __shared__ uint32_t parents[Pages::kPairs / 32], children[Pages::kPairs / 32];  // a bit per sequence
+  __shared__ int listed[kPlanThreads], after[kPlanThreads];
+  const int tid = threadIdx.x;
+  for (int w = tid; w < (D.B + 31) / 32; w += kPlanThreads) parents[w] = children[w] = 0;
+  __syncthreads();
+  for (int i = tid; i < n; i += kPlanThreads) {
+    const int s = src[i];
+    if (s >= 0 && s < D.B) atomicOr(&parents[s >> 5], 1u << (s & 31));
+  }
+  for (int i0 = 0; i0 < n; i0 += kPlanThreads) {  // whoever is listed as a child before: in an earlier round, or in front in this one
+    const int i = i0 + tid, s = i < n ? src[i] : -1, t = i < n ? dst[i] : -1;
+    listed[tid] = t;
+    __syncthreads();
     bool ok = s >= 0 && s < D.B && t >= 0 && t < D.B && s != t;
-    for (int o = 0; o < n; ++o) ok &= src[o] != t && (o >= i || dst[o] != t);
-    if (ok) ok = ctx_len[t] <= 0;
-    P.parent[i] = ok ? s : -1;
+    int ctx = 0;
+    if (ok) {
+      ctx = ctx_len[t];
+      ok = (parents[t >> 5] >> (t & 31) & 1) == 0 && (children[t >> 5] >> (t & 31) & 1) == 0;
+    }
+    for (int o = 0; o < tid && ok; ++o) ok = listed[o] != t;
+    ok &= ctx <= 0;
+    if (i < n) P.parent[i] = ok ? s : -1;
+    after[tid] = ok ? s : D.B;  // refused ones behind the others
+    __syncthreads();
+    if (t >= 0 && t < D.B) atomicOr(&children[t >> 5], 1u << (t & 31));
+    // Children of one parent side by side, so that what they take of it is read once.  The rank of each is counted, up to one round of
+    // them; longer lists stay in the caller's order.
+    int rank = i;
+    if (n <= kPlanThreads && i < n) {
+      rank = 0;
+      const int mine = after[tid];
+      for (int o = 0; o < n; ++o) rank += after[o] < mine || (after[o] == mine && o < tid);
+    }
+    if (i < n) P.order[rank] = i;
+    __syncthreads();
   }
-  __syncthreads();
   const int rows = n * D.Hkv;
-  if (deep) {  // a wave counts a row
-    for (int r = wave; r < rows; r += kPlanWaves) {
-      const int i = r / D.Hkv, s = P.parent[i];
-      int c = 0;
-      if (s >= 0) {
-        const int nb = num_blocks(D, ctx_len[s]);
-        const int32_t* row = table + ((size_t)s * D.Hkv + (r - i * D.Hkv)) * D.max_blocks;
-        for (int j = lane; j < nb; j += kWave) c += has_slot(row[j], P.n_slots);
-        c = wave_scan(c, lane);
-      }
-      if (lane == kWave - 1) P.base[r] = c;
-    }
-  } else {
-    for (int r = threadIdx.x; r < rows; r += kPlanThreads) {
-      const int i = r / D.Hkv, s = P.parent[i];
-      int c = 0;
-      if (s >= 0) {
-        const int ctx = ctx_len[s], nb = num_blocks(D, ctx);
-        if (nb > 0 && is_copied(D, false, ctx, nb, nb - 1))
-          c = has_slot(table[((size_t)s * D.Hkv + (r - i * D.Hkv)) * D.max_blocks + nb - 1], P.n_slots);
-      }
-      P.base[r] = c;
-    }
-  }
-  __syncthreads();
   long long want = 0;
   for (int r0 = 0; r0 < rows; r0 += kPlanThreads) {
-    const int r = r0 + threadIdx.x;
+    const int r = r0 + tid, i = r / D.Hkv;
+    const int s = r < rows ? P.parent[i] : -1;
+    int c = 0;
+    if (s >= 0 && deep) {
+      c = P.base[r];
+    } else if (s >= 0) {
+      const int ctx = ctx_len[s], nb = num_blocks(D, ctx);
+      if (nb > 0 && is_copied(D, false, ctx, nb, nb - 1))
+        c = has_slot(table[((size_t)s * D.Hkv + (r - i * D.Hkv)) * D.max_blocks + nb - 1], P.n_slots);
+    }
     int total;
-    const int before = plan_scan(r < rows ? P.base[r] : 0, lds, &total);
+    const int before = plan_scan(c, lds, &total);
     if (r < rows) P.base[r] = (int)want + before;
     want += total;
   }
   __syncthreads();
   const int got = want > 0 ? take_lowest(P, want, P.list, lds) : 0;
-  if (threadIdx.x == 0) P.head[0] = got;
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+  if (tid == 0) P.head[0] = got;
+  for (int i = tid; i < n; i += kPlanThreads) {
     const long long first = P.base[i * D.Hkv], end = i + 1 < n ? P.base[(i + 1) * D.Hkv] : want;
     const long long missing = end - (first > got ? first : got);
     status[i] = P.parent[i] < 0 ? -1 : missing > 0 ? (int)missing : 0;
   }
 }
 
-// Tile `from` to tile `to` in both pools, by `threads` threads of which this is `thread`: four reads of each pool in flight.
-__device__ __forceinline__ void copy_tile(char* k_pool, char* v_pool, size_t from, size_t to, int tile_bytes, int thread, int threads) {
-  for (int at = thread * 16; at < tile_bytes; at += threads * 64) {
-    uint4 k[4], v[4];
+constexpr int kTilePieces = 4;  // 16-byte pieces of each pool that a thread holds at a time
+
+// Up to 16 KiB of a tile of both pools, from byte `at` on, in the registers of a workgroup.
+struct TilePart {
+  uint4 k[kTilePieces], v[kTilePieces];
+  __device__ __forceinline__ void load(const char* k_pool, const char* v_pool, size_t tile, int at, int tile_bytes) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int o = at + u * threads * 16;
+    for (int u = 0; u < kTilePieces; ++u) {
+      const int o = at + (u * kCopyThreads + (int)threadIdx.x) * 16;
       if (o < tile_bytes) {
-        k[u] = *reinterpret_cast<const uint4*>(k_pool + from + o);
-        v[u] = *reinterpret_cast<const uint4*>(v_pool + from + o);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int o = at + u * threads * 16;
-      if (o < tile_bytes) {
-        *reinterpret_cast<uint4*>(k_pool + to + o) = k[u];
-        *reinterpret_cast<uint4*>(v_pool + to + o) = v[u];
+        k[u] = *reinterpret_cast<const uint4*>(k_pool + tile + o);
+        v[u] = *reinterpret_cast<const uint4*>(v_pool + tile + o);
       }
     }
   }
-}
+  __device__ __forceinline__ void store(char* k_pool, char* v_pool, size_t tile, int at, int tile_bytes) const {
+#pragma unroll
+    for (int u = 0; u < kTilePieces; ++u) {
+      const int o = at + (u * kCopyThreads + (int)threadIdx.x) * 16;
+      if (o < tile_bytes) {
+        *reinterpret_cast<uint4*>(k_pool + tile + o) = k[u];
+        *reinterpret_cast<uint4*>(v_pool + tile + o) = v[u];
+      }
+    }
+  }
+};
+constexpr int kPartBytes = kTilePieces * kCopyThreads * 16;
 
 constexpr int kRowPieces = 2 * kCopyThreads;  // 16-byte pieces of digests that a workgroup holds at a time
-constexpr int kForkEntries = 8;               // table entries that a tile workgroup of a deep fork takes
+constexpr int kForkBatch = 4;                 // children that a workgroup writes to
+constexpr int kForkEntries = 4;               // table entries that a tile workgroup of a deep fork takes
 
-// The first row_wgs workgroups: digests and table entries of a range of blocks of a KV head, read once and written to every child
-// of that parent in the list's order.  The others: tiles, of one child's KV head (shallow: its last block; deep: a range).
+// The first row_wgs workgroups: digests and table entries of a range of blocks of a KV head, for kForkBatch children.  The others: tiles
+// of a KV head (shallow: the last block; deep: a range), for as many.  What the children of one parent take is read once.
 __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P, int n, const int32_t* __restrict__ dst, int deep,
                                                                  int32_t* ctx_len, char* digest, int entry_bytes, int32_t* table,
                                                                  char* k_pool, char* v_pool, int tile_bytes, int stride_bytes,
-                                                                 int row_wgs, int row_blocks, int tile_wgs_per_pair) {
-  if ((int)blockIdx.x < row_wgs) {
-    const int g = blockIdx.x % D.Hkv, j0 = blockIdx.x / D.Hkv * row_blocks;
-    const int j1 = j0 + row_blocks < D.max_blocks ? j0 + row_blocks : D.max_blocks;
+                                                                 int row_wgs, int row_blocks, int parts) {
+  const int batches = (n + kForkBatch - 1) / kForkBatch;
+  const bool rows = (int)blockIdx.x < row_wgs;
+  const int w = rows ? blockIdx.x : blockIdx.x - row_wgs;
+  const int batch = w % batches, g = w / batches % D.Hkv, part = w / batches / D.Hkv;
+  const int i1 = (batch + 1) * kForkBatch < n ? (batch + 1) * kForkBatch : n;
+  int parent[kForkBatch], child[kForkBatch], fork[kForkBatch];
+#pragma unroll
+  for (int u = 0; u < kForkBatch; ++u) {
+    const int i = batch * kForkBatch + u < i1 ? P.order[batch * kForkBatch + u] : -1;
+    fork[u] = i;
+    parent[u] = i >= 0 ? P.parent[i] : -1;
+    child[u] = i >= 0 ? dst[i] : -1;
+  }
+  if (rows) {
+    const int j0 = part * row_blocks, j1 = j0 + row_blocks < D.max_blocks ? j0 + row_blocks : D.max_blocks;
     const int pieces_per_entry = entry_bytes / 16;
     int held_of = -1, nb = 0, ctx = 0, entry = -1, sharers = 0;
     bool shared = false;
@@ -245,14 +297,16 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P
       if (shared && sharers > 0) atomicAdd(P.refs + entry, sharers);
       sharers = 0;
     };
-    for (int i = 0; i < n; ++i) {
-      const int s = P.parent[i];
+#pragma unroll
+    for (int c = 0; c < kForkBatch; ++c) {
+      const int s = parent[c];
       if (s < 0) continue;
       const size_t from = (size_t)s * D.Hkv + g;
       if (s != held_of) {
         count();
         held_of = s;
         ctx = ctx_len[s];
+        entry = j < j1 ? table[from * D.max_blocks + j] : -1;
         nb = num_blocks(D, ctx);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -260,14 +314,10 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P
           if (j0 + pc / pieces_per_entry < (nb < j1 ? nb : j1))
             x[u] = *reinterpret_cast<const uint4*>(digest + (from * D.max_blocks + j0) * entry_bytes + (size_t)pc * 16);
         }
-        entry = -1;
-        if (j < j1 && j < nb) {
-          const int e = table[from * D.max_blocks + j];
-          if (has_slot(e, P.n_slots)) entry = e;
-        }
+        if (j >= nb || !has_slot(entry, P.n_slots)) entry = -1;
         shared = entry >= 0 && !is_copied(D, deep, ctx, nb, j);
       }
-      const size_t to = (size_t)dst[i] * D.Hkv + g;
+      const size_t to = (size_t)child[c] * D.Hkv + g;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int pc = threadIdx.x + u * kCopyThreads;
@@ -281,67 +331,107 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P
     count();
     return;
   }
-  const int w = blockIdx.x - row_wgs;
-  const int r = w / tile_wgs_per_pair, part = w - r * tile_wgs_per_pair;
-  const int i = r / D.Hkv, g = r - i * D.Hkv;
-  const int s = P.parent[i];
-  if (s < 0) return;
-  const int t = dst[i], ctx = ctx_len[s], nb = num_blocks(D, ctx), got = P.head[0];
-  if (g == 0 && part == 0 && threadIdx.x == 0) ctx_len[t] = ctx;
-  const int32_t* row = table + ((size_t)s * D.Hkv + g) * D.max_blocks;
-  int32_t* child = table + ((size_t)t * D.Hkv + g) * D.max_blocks;
-  int j0 = nb - 1, j1 = nb, rank = P.base[r];
-  if (deep) {
-    j0 = part * kForkEntries;
-    j1 = j0 + kForkEntries < nb ? j0 + kForkEntries : nb;
-    if (j0 >= j1) return;
-    // the row's entries with a slot in front of this range
-    __shared__ int lds[kCopyThreads / kWave];
-    int c = 0;
-    for (int j = threadIdx.x; j < j0; j += kCopyThreads) c += has_slot(row[j], P.n_slots);
-    c = wave_scan(c, lane_id());
-    if (lane_id() == kWave - 1) lds[threadIdx.x / kWave] = c;
-    __syncthreads();
+  const int got = P.head[0];
+  __shared__ int lds[kCopyThreads / kWave];
+  int held_of = -1, ctx = 0, nb = 0, before = 0;
 #pragma unroll
-    for (int v = 0; v < kCopyThreads / kWave; ++v) rank += lds[v];
-  } else if (nb == 0 || !is_copied(D, false, ctx, nb, j0)) {
-    return;
-  }
-  for (int j = j0; j < j1; ++j) {
-    const int e = row[j];
-    if (!has_slot(e, P.n_slots)) continue;
-    const int slot = rank < got ? P.list[rank] : -1;
-    ++rank;
-    if (threadIdx.x == 0) child[j] = slot;
-    if (slot >= 0) copy_tile(k_pool, v_pool, (size_t)e * stride_bytes, (size_t)slot * stride_bytes, tile_bytes, threadIdx.x, kCopyThreads);
+  for (int c0 = 0; c0 < kForkBatch; ++c0) {
+    const int s = parent[c0];
+    if (s < 0 || s == held_of) continue;  // (its children are served with the first of them)
+    held_of = s;
+    ctx = ctx_len[s];
+    nb = num_blocks(D, ctx);
+    if (g == 0 && part == 0 && threadIdx.x < kForkBatch) {
+#pragma unroll
+      for (int c = 0; c < kForkBatch; ++c)
+        if ((int)threadIdx.x == c && parent[c] == s) ctx_len[child[c]] = ctx;
+    }
+    const int32_t* row = table + ((size_t)s * D.Hkv + g) * D.max_blocks;
+    int j0 = nb - 1, j1 = nb;
+    before = 0;
+    if (deep) {
+      j0 = part * kForkEntries;
+      j1 = j0 + kForkEntries < nb ? j0 + kForkEntries : nb;
+      if (j0 >= j1) continue;
+      // the row's entries with a slot in front of this range
+      int x = 0;
+#pragma unroll 4
+      for (int j = threadIdx.x; j < j0; j += kCopyThreads) x += has_slot(row[j], P.n_slots);
+      x = wave_scan(x, lane_id());
+      __syncthreads();  // the words may still be read for the parent before
+      if (lane_id() == kWave - 1) lds[threadIdx.x / kWave] = x;
+      __syncthreads();
+#pragma unroll
+      for (int v = 0; v < kCopyThreads / kWave; ++v) before += lds[v];
+    } else if (nb == 0 || !is_copied(D, false, ctx, nb, j0)) {
+      continue;
+    }
+    for (int j = j0; j < j1; ++j) {
+      const int e = row[j];
+      if (!has_slot(e, P.n_slots)) continue;
+      int slot[kForkBatch];
+#pragma unroll
+      for (int c = 0; c < kForkBatch; ++c) {
+        slot[c] = -1;
+        if (parent[c] != s) continue;
+        const int rank = P.base[fork[c] * D.Hkv + g] + before;
+        if (rank < got) slot[c] = P.list[rank];
+        if (threadIdx.x == 0) table[((size_t)child[c] * D.Hkv + g) * D.max_blocks + j] = slot[c];
+      }
+      ++before;
+      for (int at = 0; at < tile_bytes; at += kPartBytes) {
+        TilePart T;
+        T.load(k_pool, v_pool, (size_t)e * stride_bytes, at, tile_bytes);
+#pragma unroll
+        for (int c = 0; c < kForkBatch; ++c)
+          if (slot[c] >= 0) T.store(k_pool, v_pool, (size_t)slot[c] * stride_bytes, at, tile_bytes);
+      }
+    }
   }
 }
 
 // ---------------------------------------------------------------- free
 
-// A workgroup per listed sequence: each of its entries gives its reference back, and the slot's bit falls with the last one.
-__global__ __launch_bounds__(1024) void free_kernel(Dims D, Pages P, int n, const int32_t* __restrict__ seq, int32_t* ctx_len,
-                                                    int32_t* table) {
-  const int i = blockIdx.x, b = seq[i];
+constexpr int kFreeEntries = 4 * kCopyThreads;  // table entries that a workgroup gives back
+
+// Each entry gives its reference back, and a slot's bit falls with its last one.  Several workgroups per sequence: they all read its length,
+// and the one that finds itself the last takes it away.
+__global__ __launch_bounds__(kCopyThreads) void free_kernel(Dims D, Pages P, const int32_t* __restrict__ seq, int32_t* ctx_len,
+                                                            int32_t* table) {
+  const int i = blockIdx.z, g = blockIdx.y, b = seq[i];
   if (b < 0 || b >= D.B) return;
-  int before = 0;  // a sequence that is listed twice is freed once
-  for (int o = threadIdx.x; o < i; o += blockDim.x) before |= seq[o] == b;
+  int32_t* const row = table + ((size_t)b * D.Hkv + g) * D.max_blocks;
+  int e[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int j = blockIdx.x * kFreeEntries + u * kCopyThreads + threadIdx.x;
+    e[u] = j < D.max_blocks ? row[j] : -1;
+  }
   const int nb = num_blocks(D, ctx_len[b]);
+  int before = 0;  // a sequence that is listed twice is freed once
+  for (int o = threadIdx.x; o < i; o += kCopyThreads) before |= seq[o] == b;
   if (__syncthreads_or(before)) return;
-  if (threadIdx.x == 0) ctx_len[b] = -1;
-  int32_t* rows = table + (size_t)b * D.Hkv * D.max_blocks;
-  for (int g = 0; g < D.Hkv; ++g, rows += D.max_blocks)
-    for (int j = threadIdx.x; j < D.max_blocks; j += blockDim.x) {
-      if (j < nb) {
-        const int e = rows[j];
-        if (has_slot(e, P.n_slots)) {
-          const int held = atomicSub(P.refs + e, 1);
-          if (held == 1) atomicAnd(P.used + (e >> 5), ~(1u << (e & 31)));
-          if (held <= 0) atomicAdd(P.refs + e, 1);  // nobody held it: the count stays
-        }
-      }
-      rows[j] = -1;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int j = blockIdx.x * kFreeEntries + u * kCopyThreads + threadIdx.x;
+    if (j < D.max_blocks) row[j] = -1;
+    if (j >= nb || !has_slot(e[u], P.n_slots)) e[u] = -1;
+  }
+  int held[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) held[u] = e[u] >= 0 ? atomicSub(P.refs + e[u], 1) : 2;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    if (held[u] == 1) atomicAnd(P.used + (e[u] >> 5), ~(1u << (e[u] & 31)));
+    if (held[u] <= 0) atomicAdd(P.refs + e[u], 1);  // nobody held it: the count stays
+  }
+  if (threadIdx.x == 0) {
+    const int all = gridDim.x * gridDim.y;
+    if (__hip_atomic_fetch_add(P.arrived + i, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == all - 1) {
+      P.arrived[i] = 0;
+      ctx_len[b] = -1;
     }
+  }
 }
 
 // ---------------------------------------------------------------- compaction
@@ -349,42 +439,36 @@ __global__ __launch_bounds__(1024) void free_kernel(Dims D, Pages P, int n, cons
 // Of the n_live used slots, those at n_live and beyond move into the free ones below, both in ascending order: every tile that
 // moves is read outside the compacted part and written inside it, so no move waits for another.
 // list: where they go, list2: where they are; old: the bits as they were, rank: used slots in front of each word.
+// A workgroup per 1024 slots; each of them counts all words by itself (100 000 slots: 12.5 KB), so that none waits for another.  The new bits
+// are written by the next launch, when nobody reads the old ones.
 __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(Pages P, int32_t* n_live_out) {
   __shared__ int lds[kPlanWaves];
-  const long long nw = words_of(P.n_slots);
-  int count = 0, n_live;
-  for (long long w = threadIdx.x; w < nw; w += kPlanThreads) count += __popc(P.used[w] & exists(P.n_slots, w));
-  plan_scan(count, lds, &n_live);
-  int seen = 0, above_from = 0;  // used slots before the chunk; used slots below n_live (once known)
-  // used slots below n_live: the holes there are n_live minus them
-  int below = 0;
+  const long long nw = words_of(P.n_slots), w0 = (long long)blockIdx.x * (kPlanThreads / 32);
+  int count = 0, n_live, mine = 0, before, below = 0, above_from;
   for (long long w = threadIdx.x; w < nw; w += kPlanThreads) {
-    const uint32_t bits = P.used[w] & exists(P.n_slots, w), in = exists(n_live, w);
-    below += __popc(bits & in);
+    const int c = __popc(P.used[w] & exists(P.n_slots, w));
+    count += c;
+    mine += w < w0 ? c : 0;
   }
+  plan_scan(count, lds, &n_live);
+  plan_scan(mine, lds, &before);
+  // used slots below n_live: the holes there are n_live minus them
+  for (long long w = threadIdx.x; w < nw && w * 32 < n_live; w += kPlanThreads) below += __popc(P.used[w] & exists(P.n_slots, w) & exists(n_live, w));
   plan_scan(below, lds, &above_from);
-  for (long long w0 = 0; w0 < nw; w0 += kPlanThreads) {
-    const long long w = w0 + threadIdx.x;
-    uint32_t bits = 0, in = 0;
-    if (w < nw) {
-      bits = P.used[w] & exists(P.n_slots, w);
-      in = exists(n_live, w);
-    }
-    int total;
-    const int before = seen + plan_scan(__popc(bits), lds, &total);
-    if (w < nw) {
+  const long long slot = w0 * 32 + threadIdx.x, w = slot >> 5;
+  const uint32_t bits = w < nw ? P.used[w] & exists(P.n_slots, w) : 0u, bit = 1u << (slot & 31);
+  const bool used = (bits & bit) != 0;
+  int total;
+  const int seen = before + plan_scan(used, lds, &total);  // used slots in front of this one
+  if (slot < P.n_slots) {
+    if ((slot & 31) == 0) {
       P.old[w] = bits;
-      P.rank[w] = before;
-      P.used[w] = in;
-      // slots of this word below n_live in front of it: w * 32, of which `before` are used
-      long long at = w * 32 - before;
-      for (uint32_t hole = ~bits & in; hole != 0; hole &= hole - 1) P.list[at++] = (int)(w * 32) + __ffs(hole) - 1;
-      long long m = (long long)before + __popc(bits & in) - above_from;
-      for (uint32_t out = bits & ~in; out != 0; out &= out - 1) P.list2[m++] = (int)(w * 32) + __ffs(out) - 1;
+      P.rank[w] = seen;
     }
-    seen += total;
+    if (!used && slot < n_live) P.list[slot - seen] = (int)slot;
+    if (used && slot >= n_live) P.list2[seen - above_from] = (int)slot;
   }
-  if (threadIdx.x == 0) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
     P.head[0] = n_live;
     P.head[1] = n_live - above_from;  // moves
     P.head[2] = above_from;
@@ -412,12 +496,18 @@ __global__ __launch_bounds__(kCopyThreads) void compact_move_kernel(Pages P, int
         P.refs[to] = P.refs[from];
         P.refs[from] = 0;
       }
-      copy_tile(k_pool, v_pool, (size_t)from * stride_bytes, (size_t)to * stride_bytes, tile_bytes, threadIdx.x, kCopyThreads);
+      for (int at = 0; at < tile_bytes; at += kPartBytes) {
+        TilePart T;
+        T.load(k_pool, v_pool, (size_t)from * stride_bytes, at, tile_bytes);
+        T.store(k_pool, v_pool, (size_t)to * stride_bytes, at, tile_bytes);
+      }
     }
     return;
   }
   w -= move_wgs;
   if (w < map_wgs) {
+    for (long long i = (long long)w * kCopyThreads + threadIdx.x; i < words_of(P.n_slots); i += (long long)map_wgs * kCopyThreads)
+      P.used[i] = exists(n_live, i);
     for (long long s = (long long)w * kCopyThreads + threadIdx.x; s < P.n_slots; s += (long long)map_wgs * kCopyThreads)
       slot_map[s] = slot_after(P, (int)s, n_live, above_from);
     return;
@@ -440,7 +530,7 @@ static unsigned wgs_for(long long items, unsigned most) {
 }
 
 int launch_pages_init(const Dims& D, const Pages& P, const int32_t* ctx_len, const int32_t* table, hipStream_t st) {
-  hipLaunchKernelGGL(pages_clear_kernel, dim3(wgs_for(P.n_slots, 1024)), dim3(kCopyThreads), 0, st, P);
+  hipLaunchKernelGGL(pages_clear_kernel, dim3(wgs_for(P.n_slots + Pages::kPairs, 1024)), dim3(kCopyThreads), 0, st, P);
   if (D.B > 0)
     hipLaunchKernelGGL(pages_count_kernel, dim3(wgs_for(D.max_blocks, 8), D.Hkv, D.B), dim3(kCopyThreads), 0, st, D, P, ctx_len, table);
   hipLaunchKernelGGL(pages_bits_kernel, dim3(wgs_for(words_of(P.n_slots), 1024)), dim3(kCopyThreads), 0, st, P);
@@ -457,27 +547,30 @@ int launch_fork(const Dims& D, int dtype, const Pages& P, int n, const int32_t* 
   if (n == 0) return SCOUT_OK;
   const int es = dtype == SCOUT_BF16 ? 2 : 4;
   const int entry_bytes = D.digest_kind == 1 ? D.d * 4 : 2 * D.d * es, tile_bytes = D.S * D.d * es;
+  if (deep) hipLaunchKernelGGL(fork_count_kernel, dim3(n * D.Hkv), dim3(kCopyThreads), 0, st, D, P, src, ctx_len, table);
   hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, D, P, n, src, dst, deep, ctx_len, table, status);
   const int row_blocks = kRowPieces * 16 / entry_bytes;  // 8 to 32
-  const int row_wgs = (D.max_blocks + row_blocks - 1) / row_blocks * D.Hkv;
-  const int per_pair = deep ? (D.max_blocks + kForkEntries - 1) / kForkEntries : 1;
-  const long long wgs = row_wgs + (long long)n * D.Hkv * per_pair;
-  hipLaunchKernelGGL(fork_copy_kernel, dim3((unsigned)wgs), dim3(kCopyThreads), 0, st, D, P, n, dst, deep, ctx_len,
+  const long long pairs = (long long)(n + kForkBatch - 1) / kForkBatch * D.Hkv;
+  const long long row_wgs = (D.max_blocks + row_blocks - 1) / row_blocks * pairs;
+  const int parts = deep ? (D.max_blocks + kForkEntries - 1) / kForkEntries : 1;
+  hipLaunchKernelGGL(fork_copy_kernel, dim3((unsigned)(row_wgs + pairs * parts)), dim3(kCopyThreads), 0, st, D, P, n, dst, deep, ctx_len,
                      static_cast<char*>(digest), entry_bytes, table, static_cast<char*>(k_pool), static_cast<char*>(v_pool), tile_bytes,
-                     D.tile_stride * es, row_wgs, row_blocks, per_pair);
+                     D.tile_stride * es, (int)row_wgs, row_blocks, parts);
   return launched();
 }
 
 int launch_free(const Dims& D, const Pages& P, int n, const int32_t* seq, int32_t* ctx_len, int32_t* table, hipStream_t st) {
   if (n == 0) return SCOUT_OK;
-  hipLaunchKernelGGL(free_kernel, dim3(n), dim3(1024), 0, st, D, P, n, seq, ctx_len, table);
+  hipLaunchKernelGGL(free_kernel, dim3((D.max_blocks + kFreeEntries - 1) / kFreeEntries, D.Hkv, n), dim3(kCopyThreads), 0, st, D, P, seq,
+                     ctx_len, table);
   return launched();
 }
 
 int launch_compact(const Dims& D, int dtype, const Pages& P, int32_t* table, void* k_pool, void* v_pool, int32_t* slot_map,
                    int32_t* n_live, hipStream_t st) {
   const int es = dtype == SCOUT_BF16 ? 2 : 4;
-  hipLaunchKernelGGL(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, P, n_live);
+  const long long plan_wgs = (P.n_slots + kPlanThreads - 1) / kPlanThreads;
+  hipLaunchKernelGGL(compact_plan_kernel, dim3((unsigned)(plan_wgs > 0 ? plan_wgs : 1)), dim3(kPlanThreads), 0, st, P, n_live);
   const long long entries = (long long)D.B * D.Hkv * D.max_blocks;
   const long long half = (P.n_slots + 1) / 2;  // at most so many tiles can move
   const int move_wgs = (int)(half < 1 ? 1 : half > 2048 ? 2048 : half), map_wgs = (int)wgs_for(P.n_slots, 512);
