@@ -418,14 +418,15 @@ int scout_layer_step(const scout_problem* p, const void* q, const void* digest,
 int scout_pages_bytes(int64_t n_slots, size_t* bytes);
 
 /*
- * The pages' state of a cache that is there already: counts the entries of
- * block_table that name a slot in [0, n_slots), of the first nb_b blocks of every
- * sequence.
+ * The pages' state of a cache that is there already: counts the entries of the
+ * first nb_b blocks of every sequence that name a slot in [0, n_slots).  Entries of
+ * blocks that a sequence does not have become -1: from here on every entry of a row
+ * that names a slot holds it.
  *   ctx_len      i32 [B]
- *   block_table  i32 [B][Hkv][max_blocks]
+ *   block_table  i32 [B][Hkv][max_blocks]   in/out
  *   pages        out
  */
-int scout_pages_init(const scout_problem* p, const int32_t* ctx_len, const int32_t* block_table,
+int scout_pages_init(const scout_problem* p, const int32_t* ctx_len, int32_t* block_table,
                      int64_t n_slots, void* pages, size_t pages_bytes, void* stream);
 
 /*
@@ -466,8 +467,9 @@ int fork_sequences(const scout_problem* p, int32_t n, const int32_t* src, const 
                    void* stream);
 
 /*
- * Free: the listed sequences give back their references, a slot without references
- * is free again, their table rows become -1 and their ctx_len -1.  Indices outside
+ * Free: the listed sequences give back the slots that their table rows name, all
+ * max_blocks of a row; a slot without references is free again, the rows become -1
+ * and their ctx_len -1.  Indices outside
  * [0, B) are skipped, a sequence that is listed twice is freed once.
  *   seq  i32 [n], n <= B  DEVICE
  */

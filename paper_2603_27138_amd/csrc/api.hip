@@ -38,7 +38,7 @@ int launch_step(const Dims&, int, const void*, const void*, const int32_t*, cons
 int launch_merge(const Dims&, int, const float*, const float*, const float*, const float*,
                  const float*, const float*, void*, float*, hipStream_t);
 
-int launch_pages_init(const Dims&, const Pages&, const int32_t*, const int32_t*, hipStream_t);
+int launch_pages_init(const Dims&, const Pages&, const int32_t*, int32_t*, hipStream_t);
 int launch_reserve(const Dims&, const Pages&, const int32_t*, int32_t*, int32_t*, hipStream_t);
 int launch_fork(const Dims&, int, const Pages&, int, const int32_t*, const int32_t*, int, int32_t*, void*, int32_t*, void*, void*,
                 int32_t*, hipStream_t);
@@ -647,7 +647,7 @@ int scout_pages_bytes(int64_t n_slots, size_t* bytes) {
   return SCOUT_OK;
 }
 
-int scout_pages_init(const scout_problem* p, const int32_t* ctx_len, const int32_t* block_table, int64_t n_slots, void* pages,
+int scout_pages_init(const scout_problem* p, const int32_t* ctx_len, int32_t* block_table, int64_t n_slots, void* pages,
                      size_t pages_bytes, void* stream) {
   Dims D;
   Pages P;

@@ -14,7 +14,6 @@ struct Pages {
   int32_t* base;    // [kPairs] first rank of a pair or sequence
   int32_t* parent;  // [kPairs] of a fork, -1 where it is refused
   int32_t* order;   // [kPairs] forks, those of one parent side by side
-  int32_t* arrived; // [kPairs] workgroups that are done with a sequence; zero between the calls
   int32_t* list;    // [n_slots] slots taken, or the holes that a compaction fills
   int32_t* list2;   // [n_slots] slots that a compaction empties
   uint32_t* old;    // [words] used before a compaction
@@ -23,7 +22,7 @@ struct Pages {
 
   static constexpr int kPairs = 65536;
   static long long up(long long n) { return (n + 63) / 64 * 64; }  // sections start at 256 bytes
-  static long long words(long long n_slots) { return 3 * up(n_slots) + 3 * up(words_of(n_slots)) + 64 + 4 * kPairs; }
+  static long long words(long long n_slots) { return 3 * up(n_slots) + 3 * up(words_of(n_slots)) + 64 + 3 * kPairs; }
 
   static Pages at(void* buffer, long long n_slots) {
     Pages P;
@@ -39,7 +38,6 @@ struct Pages {
     P.base = next(kPairs);
     P.parent = next(kPairs);
     P.order = next(kPairs);
-    P.arrived = next(kPairs);
     P.list = next(n_slots);
     P.list2 = next(n_slots);
     P.old = reinterpret_cast<uint32_t*>(next(words_of(n_slots)));

@@ -55,23 +55,31 @@ __device__ __forceinline__ uint32_t exists(long long n_slots, long long w) {
 // become used with one reference each.  The whole planning workgroup calls this.
 __device__ int take_lowest(const Pages& P, long long want, int32_t* list, int* lds) {
   const long long nw = words_of(P.n_slots);
+  const int lane = lane_id();
   long long got = 0;
   for (long long w0 = 0; w0 < nw && got < want; w0 += kPlanThreads) {
     const long long w = w0 + threadIdx.x;
     uint32_t free_bits = 0;
     if (w < nw) free_bits = ~P.used[w] & exists(P.n_slots, w);
     int total;
-    long long at = got + plan_scan(__popc(free_bits), lds, &total);
-    uint32_t taken = 0;
-    while (free_bits != 0 && at < want) {
-      const uint32_t bit = free_bits & -free_bits;
-      const int slot = (int)(w * 32) + __ffs(bit) - 1;
-      list[at++] = slot;
-      P.refs[slot] = 1;
-      taken |= bit;
-      free_bits ^= bit;
-    }
+    const long long at = got + plan_scan(__popc(free_bits), lds, &total);
+    uint32_t taken = at < want ? free_bits : 0u;
+    for (long long more = taken ? at + __popc(taken) - want : 0; more > 0; --more) taken &= ~(0x80000000u >> __clz(taken));  // the highest ones stay
     if (taken) P.used[w] |= taken;
+    // Two words of the wave at a time, a lane per slot, so that neighbours are stored together (a word per lane: five times as long).
+    if (__ballot(taken != 0) != 0) {
+#pragma unroll 4
+      for (int k = 0; k < kWave; k += 2) {
+        const int from = k + lane / 32;
+        const uint32_t bits = __shfl(taken, from), bit = 1u << (lane & 31);
+        const int first = __shfl((int)at, from);
+        if (bits & bit) {
+          const int slot = (int)((w0 + (threadIdx.x - lane) + from) * 32) + (lane & 31);
+          list[first + __popc(bits & (bit - 1))] = slot;
+          P.refs[slot] = 1;
+        }
+      }
+    }
     got += total;
   }
   return (int)(got < want ? got : want);
@@ -84,15 +92,15 @@ __device__ __forceinline__ bool has_slot(int entry, long long n_slots) { return 
 __global__ __launch_bounds__(kCopyThreads) void pages_clear_kernel(Pages P) {
   const long long n = P.n_slots, step = (long long)gridDim.x * kCopyThreads;
   for (long long i = (long long)blockIdx.x * kCopyThreads + threadIdx.x; i < n; i += step) P.refs[i] = 0;
-  for (long long i = (long long)blockIdx.x * kCopyThreads + threadIdx.x; i < Pages::kPairs; i += step) P.arrived[i] = 0;
 }
 
-__global__ __launch_bounds__(kCopyThreads) void pages_count_kernel(Dims D, Pages P, const int32_t* __restrict__ ctx_len,
-                                                                   const int32_t* __restrict__ table) {
+__global__ __launch_bounds__(kCopyThreads) void pages_count_kernel(Dims D, Pages P, const int32_t* __restrict__ ctx_len, int32_t* table) {
   const int pair = grid_pair(), nb = num_blocks(D, ctx_len[blockIdx.z]);
-  for (int j = blockIdx.x * kCopyThreads + threadIdx.x; j < nb; j += gridDim.x * kCopyThreads) {
-    const int e = table[(size_t)pair * D.max_blocks + j];
-    if (has_slot(e, P.n_slots)) atomicAdd(P.refs + e, 1);
+  int32_t* const row = table + (size_t)pair * D.max_blocks;
+  for (int j = blockIdx.x * kCopyThreads + threadIdx.x; j < D.max_blocks; j += gridDim.x * kCopyThreads) {
+    const int e = row[j];
+    if (j >= nb) row[j] = -1;
+    else if (has_slot(e, P.n_slots)) atomicAdd(P.refs + e, 1);
   }
 }
 
@@ -190,8 +198,11 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(Dims D, Pages P
       ctx = ctx_len[t];
       ok = (parents[t >> 5] >> (t & 31) & 1) == 0 && (children[t >> 5] >> (t & 31) & 1) == 0;
     }
-    for (int o = 0; o < tid && ok; ++o) ok = listed[o] != t;
-    ok &= ctx <= 0;
+    const int round = n - i0 < kPlanThreads ? n - i0 : kPlanThreads;
+    int twice = 0;
+#pragma unroll 8
+    for (int o = 0; o < round; ++o) twice |= (listed[o] == t) & (o < tid);
+    ok &= ctx <= 0 && !twice;
     if (i < n) P.parent[i] = ok ? s : -1;
     after[tid] = ok ? s : D.B;  // refused ones behind the others
     __syncthreads();
@@ -202,6 +213,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(Dims D, Pages P
     if (n <= kPlanThreads && i < n) {
       rank = 0;
       const int mine = after[tid];
+#pragma unroll 8
       for (int o = 0; o < n; ++o) rank += after[o] < mine || (after[o] == mine && o < tid);
     }
     if (i < n) P.order[rank] = i;
@@ -235,18 +247,21 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(Dims D, Pages P
   }
 }
 
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;  // (a copy of HIP's uint4 is four stores: half the rate)
+
 constexpr int kTilePieces = 4;  // 16-byte pieces of each pool that a thread holds at a time
 
-// Up to 16 KiB of a tile of both pools, from byte `at` on, in the registers of a workgroup.
+// Up to 16 KiB of a tile of both pools, from byte `at` on, in the registers of a workgroup.  The stores pass the caches by: what they
+// leave is read by later steps (a deep fork of four sequences of 32k tokens, 269 MB of tiles: 61 us, 90 through the caches).
 struct TilePart {
-  uint4 k[kTilePieces], v[kTilePieces];
+  u32x4 k[kTilePieces], v[kTilePieces];
   __device__ __forceinline__ void load(const char* k_pool, const char* v_pool, size_t tile, int at, int tile_bytes) {
 #pragma unroll
     for (int u = 0; u < kTilePieces; ++u) {
       const int o = at + (u * kCopyThreads + (int)threadIdx.x) * 16;
       if (o < tile_bytes) {
-        k[u] = *reinterpret_cast<const uint4*>(k_pool + tile + o);
-        v[u] = *reinterpret_cast<const uint4*>(v_pool + tile + o);
+        k[u] = *reinterpret_cast<const u32x4*>(k_pool + tile + o);
+        v[u] = *reinterpret_cast<const u32x4*>(v_pool + tile + o);
       }
     }
   }
@@ -255,8 +270,8 @@ struct TilePart {
     for (int u = 0; u < kTilePieces; ++u) {
       const int o = at + (u * kCopyThreads + (int)threadIdx.x) * 16;
       if (o < tile_bytes) {
-        *reinterpret_cast<uint4*>(k_pool + tile + o) = k[u];
-        *reinterpret_cast<uint4*>(v_pool + tile + o) = v[u];
+        __builtin_nontemporal_store(k[u], reinterpret_cast<u32x4*>(k_pool + tile + o));
+        __builtin_nontemporal_store(v[u], reinterpret_cast<u32x4*>(v_pool + tile + o));
       }
     }
   }
@@ -272,11 +287,10 @@ constexpr int kForkEntries = 4;               // table entries that a tile workg
 __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P, int n, const int32_t* __restrict__ dst, int deep,
                                                                  int32_t* ctx_len, char* digest, int entry_bytes, int32_t* table,
                                                                  char* k_pool, char* v_pool, int tile_bytes, int stride_bytes,
-                                                                 int row_wgs, int row_blocks, int parts) {
-  const int batches = (n + kForkBatch - 1) / kForkBatch;
+                                                                 int row_wgs, int row_blocks, int row_parts, int parts) {
   const bool rows = (int)blockIdx.x < row_wgs;
   const int w = rows ? blockIdx.x : blockIdx.x - row_wgs;
-  const int batch = w % batches, g = w / batches % D.Hkv, part = w / batches / D.Hkv;
+  const int of = rows ? row_parts : parts, part = w % of, g = w / of % D.Hkv, batch = w / of / D.Hkv;
   const int i1 = (batch + 1) * kForkBatch < n ? (batch + 1) * kForkBatch : n;
   int parent[kForkBatch], child[kForkBatch], fork[kForkBatch];
 #pragma unroll
@@ -291,7 +305,7 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P
     const int pieces_per_entry = entry_bytes / 16;
     int held_of = -1, nb = 0, ctx = 0, entry = -1, sharers = 0;
     bool shared = false;
-    uint4 x[2];
+    u32x4 x[2];
     const int j = j0 + threadIdx.x;
     auto count = [&]() {
       if (shared && sharers > 0) atomicAdd(P.refs + entry, sharers);
@@ -312,7 +326,7 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P
         for (int u = 0; u < 2; ++u) {
           const int pc = threadIdx.x + u * kCopyThreads;
           if (j0 + pc / pieces_per_entry < (nb < j1 ? nb : j1))
-            x[u] = *reinterpret_cast<const uint4*>(digest + (from * D.max_blocks + j0) * entry_bytes + (size_t)pc * 16);
+            x[u] = *reinterpret_cast<const u32x4*>(digest + (from * D.max_blocks + j0) * entry_bytes + (size_t)pc * 16);
         }
         if (j >= nb || !has_slot(entry, P.n_slots)) entry = -1;
         shared = entry >= 0 && !is_copied(D, deep, ctx, nb, j);
@@ -322,7 +336,7 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P
       for (int u = 0; u < 2; ++u) {
         const int pc = threadIdx.x + u * kCopyThreads;
         if (j0 + pc / pieces_per_entry < (nb < j1 ? nb : j1))
-          *reinterpret_cast<uint4*>(digest + (to * D.max_blocks + j0) * entry_bytes + (size_t)pc * 16) = x[u];
+          *reinterpret_cast<u32x4*>(digest + (to * D.max_blocks + j0) * entry_bytes + (size_t)pc * 16) = x[u];
       }
       // an entry whose tile is copied is written by the workgroup that copies it
       if (j < j1 && !(entry >= 0 && !shared)) table[to * D.max_blocks + j] = entry;
@@ -392,46 +406,45 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P
 
 // ---------------------------------------------------------------- free
 
-constexpr int kFreeEntries = 4 * kCopyThreads;  // table entries that a workgroup gives back
+constexpr int kFreeBatch = 8, kFreeBlocks = 64;  // sequences and blocks that a workgroup looks at, a thread for each
 
-// Each entry gives its reference back, and a slot's bit falls with its last one.  Several workgroups per sequence: they all read its length,
-// and the one that finds itself the last takes it away.
-__global__ __launch_bounds__(kCopyThreads) void free_kernel(Dims D, Pages P, const int32_t* __restrict__ seq, int32_t* ctx_len,
-                                                            int32_t* table) {
-  const int i = blockIdx.z, g = blockIdx.y, b = seq[i];
-  if (b < 0 || b >= D.B) return;
-  int32_t* const row = table + ((size_t)b * D.Hkv + g) * D.max_blocks;
-  int e[4];
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int j = blockIdx.x * kFreeEntries + u * kCopyThreads + threadIdx.x;
-    e[u] = j < D.max_blocks ? row[j] : -1;
+// Each entry gives its reference back, and a slot's bit falls with its last one.  Sequences that share a slot, as forks of one parent do,
+// give back together, with one addition.
+__global__ __launch_bounds__(kFreeBatch* kFreeBlocks) void free_kernel(Dims D, Pages P, int n, const int32_t* __restrict__ seq,
+                                                                       int32_t* ctx_len, int32_t* table) {
+  __shared__ int again[kFreeBatch], named[kFreeBatch][kFreeBlocks];
+  const int u = threadIdx.x / kFreeBlocks, jj = threadIdx.x % kFreeBlocks, j = blockIdx.x * kFreeBlocks + jj;  // a wave has one u
+  const int g = blockIdx.y, i0 = blockIdx.z * kFreeBatch, i = i0 + u;
+  int b = i < n ? seq[i] : -1;
+  if (b >= D.B) b = -1;
+  if (threadIdx.x < kFreeBatch) again[threadIdx.x] = 0;
+  __syncthreads();
+  int32_t* const entry = table + ((size_t)(b < 0 ? 0 : b) * D.Hkv + g) * D.max_blocks + j;
+  int e = -1;
+  if (b >= 0) {
+    if (j < D.max_blocks) e = *entry;
+    for (int o = jj; o < i; o += kFreeBlocks)  // a sequence that is listed twice is freed once
+      if (seq[o] == b) again[u] = 1;
   }
-  const int nb = num_blocks(D, ctx_len[b]);
-  int before = 0;  // a sequence that is listed twice is freed once
-  for (int o = threadIdx.x; o < i; o += kCopyThreads) before |= seq[o] == b;
-  if (__syncthreads_or(before)) return;
+  __syncthreads();
+  if (again[u]) b = -1;
+  if (b < 0 || !has_slot(e, P.n_slots)) e = -1;
+  named[u][jj] = e;
+  if (b >= 0 && j < D.max_blocks) *entry = -1;
+  __syncthreads();
+  int gives = e >= 0;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int j = blockIdx.x * kFreeEntries + u * kCopyThreads + threadIdx.x;
-    if (j < D.max_blocks) row[j] = -1;
-    if (j >= nb || !has_slot(e[u], P.n_slots)) e[u] = -1;
+  for (int v = 0; v < kFreeBatch; ++v) {
+    const bool same = named[v][jj] == e;
+    if (v < u && same) gives = 0;
+    if (v > u && same && gives) ++gives;
   }
-  int held[4];
-#pragma unroll
-  for (int u = 0; u < 4; ++u) held[u] = e[u] >= 0 ? atomicSub(P.refs + e[u], 1) : 2;
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    if (held[u] == 1) atomicAnd(P.used + (e[u] >> 5), ~(1u << (e[u] & 31)));
-    if (held[u] <= 0) atomicAdd(P.refs + e[u], 1);  // nobody held it: the count stays
+  if (gives) {
+    const int held = atomicSub(P.refs + e, gives);
+    if (held < gives) atomicAdd(P.refs + e, gives - (held > 0 ? held : 0));  // fewer held it: the count ends at zero
+    if (held > 0 && held <= gives) atomicAnd(P.used + (e >> 5), ~(1u << (e & 31)));
   }
-  if (threadIdx.x == 0) {
-    const int all = gridDim.x * gridDim.y;
-    if (__hip_atomic_fetch_add(P.arrived + i, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == all - 1) {
-      P.arrived[i] = 0;
-      ctx_len[b] = -1;
-    }
-  }
+  if (blockIdx.x == 0 && g == 0 && jj == 0 && b >= 0) ctx_len[b] = -1;
 }
 
 // ---------------------------------------------------------------- compaction
@@ -529,8 +542,8 @@ static unsigned wgs_for(long long items, unsigned most) {
   return (unsigned)(w < 1 ? 1 : w > most ? most : w);
 }
 
-int launch_pages_init(const Dims& D, const Pages& P, const int32_t* ctx_len, const int32_t* table, hipStream_t st) {
-  hipLaunchKernelGGL(pages_clear_kernel, dim3(wgs_for(P.n_slots + Pages::kPairs, 1024)), dim3(kCopyThreads), 0, st, P);
+int launch_pages_init(const Dims& D, const Pages& P, const int32_t* ctx_len, int32_t* table, hipStream_t st) {
+  hipLaunchKernelGGL(pages_clear_kernel, dim3(wgs_for(P.n_slots, 1024)), dim3(kCopyThreads), 0, st, P);
   if (D.B > 0)
     hipLaunchKernelGGL(pages_count_kernel, dim3(wgs_for(D.max_blocks, 8), D.Hkv, D.B), dim3(kCopyThreads), 0, st, D, P, ctx_len, table);
   hipLaunchKernelGGL(pages_bits_kernel, dim3(wgs_for(words_of(P.n_slots), 1024)), dim3(kCopyThreads), 0, st, P);
@@ -551,18 +564,19 @@ int launch_fork(const Dims& D, int dtype, const Pages& P, int n, const int32_t* 
   hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, D, P, n, src, dst, deep, ctx_len, table, status);
   const int row_blocks = kRowPieces * 16 / entry_bytes;  // 8 to 32
   const long long pairs = (long long)(n + kForkBatch - 1) / kForkBatch * D.Hkv;
-  const long long row_wgs = (D.max_blocks + row_blocks - 1) / row_blocks * pairs;
+  const int row_parts = (D.max_blocks + row_blocks - 1) / row_blocks;
+  const long long row_wgs = row_parts * pairs;
   const int parts = deep ? (D.max_blocks + kForkEntries - 1) / kForkEntries : 1;
   hipLaunchKernelGGL(fork_copy_kernel, dim3((unsigned)(row_wgs + pairs * parts)), dim3(kCopyThreads), 0, st, D, P, n, dst, deep, ctx_len,
                      static_cast<char*>(digest), entry_bytes, table, static_cast<char*>(k_pool), static_cast<char*>(v_pool), tile_bytes,
-                     D.tile_stride * es, (int)row_wgs, row_blocks, parts);
+                     D.tile_stride * es, (int)row_wgs, row_blocks, row_parts, parts);
   return launched();
 }
 
 int launch_free(const Dims& D, const Pages& P, int n, const int32_t* seq, int32_t* ctx_len, int32_t* table, hipStream_t st) {
   if (n == 0) return SCOUT_OK;
-  hipLaunchKernelGGL(free_kernel, dim3((D.max_blocks + kFreeEntries - 1) / kFreeEntries, D.Hkv, n), dim3(kCopyThreads), 0, st, D, P, seq,
-                     ctx_len, table);
+  hipLaunchKernelGGL(free_kernel, dim3((D.max_blocks + kFreeBlocks - 1) / kFreeBlocks, D.Hkv, (n + kFreeBatch - 1) / kFreeBatch),
+                     dim3(kFreeBatch * kFreeBlocks), 0, st, D, P, n, seq, ctx_len, table);
   return launched();
 }
 

@@ -21,7 +21,8 @@ class Book:
     def init(self):
         self.refs = np.zeros(self.n_slots, np.int32)
         for b in range(len(self.ctx)):
-            for e in self.table[b, :, :self.blocks(b)].ravel():
+            self.table[b, :, self.blocks(b):] = -1
+            for e in self.table[b].ravel():
                 if self.valid(e):
                     self.refs[e] += 1
 
@@ -81,7 +82,7 @@ class Book:
 
     def free(self, seq):
         for b in dict.fromkeys(x for x in seq if 0 <= x < len(self.ctx)):
-            for e in self.table[b, :, :self.blocks(b)].ravel():
+            for e in self.table[b].ravel():
                 if self.valid(e) and self.refs[e] > 0:
                     self.refs[e] -= 1
             self.table[b], self.ctx[b] = -1, -1

@@ -222,6 +222,55 @@ def test_entries_that_name_no_slot():
     c.free([2])
 
 
+def test_entries_beyond_the_last_block():
+    """They are no blocks to begin with; an entry that a caller leaves behind there (a sequence cut short) is given back with the rest."""
+    rng = np.random.default_rng(12)
+    c = Cache(rng, 3, 2, 16, 64, torch.bfloat16, 5, 40, [40, -1, 16], share=1.0)
+    c.table[0, :, 3:] = c.book.table[0, :, 3:] = 39
+    c.table[1] = c.book.table[1] = 5
+    B.pages_init(c.p, c.ctx, c.table, c.n_slots, c.pages)
+    c.book.init()
+    c.check("init")
+    c.ctx[0] = c.book.ctx[0] = 20
+    c.fork([0], [1])
+    c.free([0, 1])
+    assert c.book.refs.sum() == 2
+
+
+def test_shared_slots_given_back_together():
+    """Forks of two parents freed in lists that mix them, and a slot that several entries of one sequence name."""
+    rng = np.random.default_rng(13)
+    c = Cache(rng, 30, 1, 16, 64, torch.bfloat16, 4, 64, [50, 64] + [-1] * 28, share=1.0)
+    c.fork([0, 1] * 10, list(range(2, 22)))
+    c.fork([0] * 5, list(range(22, 27)))
+    c.free([2, 3, 4, 5, 6, 7, 8, 9, 10, 25, 11, 2, 3])
+    c.free([0])
+    c.free(list(range(30)))
+    assert not c.book.refs.any()
+    c.table[4] = c.book.table[4] = 7
+    c.ctx[4] = c.book.ctx[4] = 64
+    B.pages_init(c.p, c.ctx, c.table, c.n_slots, c.pages)
+    c.book.init()
+    c.fork([4], [5])
+    c.free([4])
+    c.free([5])
+
+
+@pytest.mark.parametrize("n", [40, 1500])
+def test_long_lists(n):
+    """More forks than one round of the plan looks at, children listed twice within and across rounds."""
+    rng = np.random.default_rng(n)
+    rows = 2 * n + 3
+    c = Cache(rng, rows, 1, 16, 64, torch.bfloat16, 3, 3000, [33, 20, -1] + [-1] * (2 * n), share=1.0)
+    dst = list(range(3, 3 + n))
+    dst[n // 3], dst[-1] = 5, 3
+    src = rng.integers(0, 2, n).tolist()
+    status = c.fork(src, dst)
+    assert (status == -1).sum() == 2
+    c.free(rng.integers(0, rows, n).tolist())
+    c.compact()
+
+
 def test_empty_lists_and_a_side_stream():
     rng = np.random.default_rng(9)
     c = Cache(rng, 4, 2, 32, 128, torch.bfloat16, 4, 64, [100, -1, -1, 31])
