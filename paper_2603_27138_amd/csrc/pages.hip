@@ -280,14 +280,13 @@ constexpr int kPartBytes = kTilePieces * kCopyThreads * 16;
 
 constexpr int kRowPieces = 2 * kCopyThreads;  // 16-byte pieces of digests that a workgroup holds at a time
 constexpr int kForkBatch = 4;                 // children that a workgroup writes to
-constexpr int kForkEntries = 4;               // table entries that a tile workgroup of a deep fork takes
 
 // The first row_wgs workgroups: digests and table entries of a range of blocks of a KV head, for kForkBatch children.  The others: tiles
 // of a KV head (shallow: the last block; deep: a range), for as many.  What the children of one parent take is read once.
 __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P, int n, const int32_t* __restrict__ dst, int deep,
                                                                  int32_t* ctx_len, char* digest, int entry_bytes, int32_t* table,
                                                                  char* k_pool, char* v_pool, int tile_bytes, int stride_bytes,
-                                                                 int row_wgs, int row_blocks, int row_parts, int parts) {
+                                                                 int row_wgs, int row_blocks, int row_parts, int parts, int entries) {
   const bool rows = (int)blockIdx.x < row_wgs;
   const int w = rows ? blockIdx.x : blockIdx.x - row_wgs;
   const int of = rows ? row_parts : parts, part = w % of, g = w / of % D.Hkv, batch = w / of / D.Hkv;
@@ -364,8 +363,8 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P
     int j0 = nb - 1, j1 = nb;
     before = 0;
     if (deep) {
-      j0 = part * kForkEntries;
-      j1 = j0 + kForkEntries < nb ? j0 + kForkEntries : nb;
+      j0 = part * entries;
+      j1 = j0 + entries < nb ? j0 + entries : nb;
       if (j0 >= j1) continue;
       // the row's entries with a slot in front of this range
       int x = 0;
@@ -566,10 +565,13 @@ int launch_fork(const Dims& D, int dtype, const Pages& P, int n, const int32_t* 
   const long long pairs = (long long)(n + kForkBatch - 1) / kForkBatch * D.Hkv;
   const int row_parts = (D.max_blocks + row_blocks - 1) / row_blocks;
   const long long row_wgs = row_parts * pairs;
-  const int parts = deep ? (D.max_blocks + kForkEntries - 1) / kForkEntries : 1;
+  // Table entries that a tile workgroup of a deep fork takes, one after the other: one where that gives no more workgroups than run at a
+  // time (2 heads of 65 blocks: 5.3 us for the launch, 8.6 with four), else four, which share the way to their first tile.
+  const int entries = pairs * D.max_blocks <= 2048 ? 1 : 4;
+  const int parts = deep ? (D.max_blocks + entries - 1) / entries : 1;
   hipLaunchKernelGGL(fork_copy_kernel, dim3((unsigned)(row_wgs + pairs * parts)), dim3(kCopyThreads), 0, st, D, P, n, dst, deep, ctx_len,
                      static_cast<char*>(digest), entry_bytes, table, static_cast<char*>(k_pool), static_cast<char*>(v_pool), tile_bytes,
-                     D.tile_stride * es, (int)row_wgs, row_blocks, row_parts, parts);
+                     D.tile_stride * es, (int)row_wgs, row_blocks, row_parts, parts, entries);
   return launched();
 }
 
