@@ -18,7 +18,7 @@ struct PrefixItem {
 struct PrefixPlan {
   static constexpr int kStampWords = 12;
   int32_t* stamp;    // what the plan was made for
-  int32_t* head;     // [0] items, [1] most splits of a row
+  int32_t* head;     // [0] items
   int32_t* splits;   // [B] partials of a sequence's rows; 0: no prefix
   int32_t* member;   // [B] sequences, prefix by prefix
   PrefixItem* item;  // [max_items]

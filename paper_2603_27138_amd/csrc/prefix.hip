@@ -36,8 +36,7 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PrefixPlan P,
   // of each prefix: its sequences, how many of them have been put in the list, where its part of the list starts, its tokens, its
   // first item
   __shared__ int count[kMaxPrefixes], placed[kMaxPrefixes], first[kMaxPrefixes], len[kMaxPrefixes], base[kMaxPrefixes + 1];
-  __shared__ long long cost[kMaxPrefixSplits];
-  __shared__ int chunk_lds, longest_lds;
+  __shared__ int chunk_lds, longest_lds, best_lds;
   const int t = threadIdx.x;
   for (int p = t; p < n_prefix; p += kPlanThreads) {
     const int n = prefix_len[p];
@@ -71,30 +70,37 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PrefixPlan P,
     const int n = round_up((longest + c) / (c + 1), shape.granule);
     return n > shape.granule ? n : shape.granule;
   };
-  if (t < kMaxPrefixSplits) {
+  static_assert(kMaxPrefixSplits == kWave, "a candidate, and a split, per lane");
+  if (t < kWave) {
     const int c = chunk_of(t);
     long long items = 0;
     for (int p = 0; p < n_prefix; ++p) items += (long long)tiles_of(p) * Hkv * splits_of(len[p], c);
     const long long rounds = (items + shape.slots - 1) / shape.slots;
-    cost[t] = items > P.max_items ? 1ll << 62 : rounds * (c + shape.head_cost);
+    long long cost = items > P.max_items ? 1ll << 62 : rounds * (c + shape.head_cost);  // without splits the items always fit
+    int best = t;
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) {  // the lowest cost, of equal ones the fewest splits
+      const long long other = __shfl_xor(cost, s);
+      const int who = __shfl_xor(best, s);
+      if (other < cost || (other == cost && who < best)) {
+        cost = other;
+        best = who;
+      }
+    }
+    if (t == 0) best_lds = best;
   }
   __syncthreads();
   if (t == 0) {
-    int best = 0;  // without splits the items always fit
-    for (int c = 1; c < kMaxPrefixSplits; ++c)
-      if (cost[c] < cost[best]) best = c;
+    const int best = best_lds;
     const int chunk = chunk_of(best);
-    int at = 0, most = 1;
+    int at = 0;
     for (int p = 0; p < n_prefix; ++p) {
-      const int s = splits_of(len[p], chunk);
       base[p] = at;
-      at += tiles_of(p) * Hkv * s;
-      most = s > most ? s : most;
+      at += tiles_of(p) * Hkv * splits_of(len[p], chunk);
     }
     base[n_prefix] = at;
     chunk_lds = chunk;
     P.head[0] = at;
-    P.head[1] = most;
   }
   if (t < PrefixPlan::kStampWords) P.stamp[t] = stamp.w[t];
   __syncthreads();
@@ -150,7 +156,7 @@ struct PrefixWork {
   long long n_slots;
   const void *q, *k_pool, *v_pool;
   const int32_t* table;  // [n_prefix][Hkv][prefix_blocks]
-  float *po, *pm, *pl;   // partials [B * Hq][splits of the plan]: unnormalised sums, maximum in base-2 units, sum
+  float *po, *pm, *pl;   // partials [B * Hq][kMaxPrefixSplits]: unnormalised sums, maximum in base-2 units, sum
 };
 
 __device__ __forceinline__ bool made_for(const PrefixPlan& P, const PrefixStamp& stamp) {
@@ -335,7 +341,6 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(Pref
     issue_unit<DT, DH>(T, W.k_pool, W.v_pool, e, ln, kg);
   }
   // the waves' partials of 16 rows at a time
-  const int stride = P.head[1];
   constexpr int AREA = 16 * ROW + 32, Q = DH / 2;
 #pragma unroll
   for (int t = 0; t < NQ; ++t) {
@@ -370,7 +375,7 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(Pref
         o[1] += f * y[1];
         sum += f * base[16 * ROW + 16 + h];
       }
-      const size_t at = (size_t)query_row(P, W, it, t * 16 + h) * stride + it.split;
+      const size_t at = (size_t)query_row(P, W, it, t * 16 + h) * kMaxPrefixSplits + it.split;
       *reinterpret_cast<f32x2*>(W.po + at * DH + c) = o;
       if (c == 0) {
         W.pm[at] = M;
@@ -726,7 +731,7 @@ __global__ __launch_bounds__(WM* WN* kWave) void prefix_wide_kernel(PrefixPlan P
     }
   }
   if (!real) return;
-  const size_t to = out_row * P.head[1] + it.split;
+  const size_t to = out_row * kMaxPrefixSplits + it.split;
 #pragma unroll
   for (int d = 0; d < L::DT; ++d)
 #pragma unroll
@@ -763,14 +768,24 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(PrefixPlan P, Prefi
     lb = E.l_b[row];
     ob = *reinterpret_cast<const typename Channels<N>::f_any*>(E.o_b + (size_t)row * DH + c);
   }
-  int n = 0, stride = 1;
-  if (made_for(P, stamp)) {
-    n = P.splits[row / W.Hq];
-    stride = P.head[1];
-  }
-  const size_t at = (size_t)row * stride;
-  float ms = lane < n ? W.pm[at + lane] : -INFINITY;
-  float ls = lane < n ? W.pl[at + lane] : 0.0f;
+  // In the first trip: how many splits there are, all that they say, and the sums of the first ones.
+  const size_t at = (size_t)row * kMaxPrefixSplits;
+  constexpr int TRIP = 16;  // splits requested at a time
+  float ms = W.pm[at + lane], ls = W.pl[at + lane];
+  const __amdgpu_buffer_rsrc_t sums = __builtin_amdgcn_make_buffer_rsrc(W.po + at * DH, 0, kMaxPrefixSplits * DH * 4, 0x00020000);
+  chans x[TRIP];
+  auto request = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < TRIP; ++u) {
+      const int off = ((s0 + u) * DH + c) * 4;
+      if constexpr (N == 2) x[u] = __builtin_bit_cast(chans, __builtin_amdgcn_raw_buffer_load_b64(sums, off, 0, 0));
+      else x[u][0] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sums, off, 0, 0));
+    }
+  };
+  request(0);
+  const int n = made_for(P, stamp) ? P.splits[row / W.Hq] : 0;
+  ms = lane < n ? ms : -INFINITY;
+  ls = lane < n ? ls : 0.0f;
   float M = ms;
 #pragma unroll
   for (int s = 1; s < kWave; s <<= 1) M = fmaxf(M, __shfl_xor(M, s));
@@ -779,20 +794,12 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(PrefixPlan P, Prefi
 #pragma unroll
   for (int s = 1; s < kWave; s <<= 1) ls += __shfl_xor(ls, s);
   chans o{};
-  constexpr int TRIP = 16;  // splits requested at a time
-  const __amdgpu_buffer_rsrc_t sums = __builtin_amdgcn_make_buffer_rsrc(W.po + at * DH, 0, n * DH * 4, 0x00020000);  // beyond: zeros
   for (int s0 = 0; s0 < n; s0 += TRIP) {
-    chans x[TRIP];
-#pragma unroll
-    for (int u = 0; u < TRIP; ++u) {
-      const int off = ((s0 + u) * DH + c) * 4;
-      if constexpr (N == 2) x[u] = __builtin_bit_cast(chans, __builtin_amdgcn_raw_buffer_load_b64(sums, off, 0, 0));
-      else x[u][0] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sums, off, 0, 0));
-    }
+    if (s0 > 0) request(s0);
 #pragma unroll
     for (int u = 0; u < TRIP; ++u) {
       const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s0 + u));
-      if (w != 0.0f) o += w * x[u];  // a split without tokens has no weight
+      if (w != 0.0f) o += w * x[u];  // a split without tokens has no weight, and what lies beyond the last one none either
     }
   }
   // The two partials as one.  A side without tokens (sum zero) has no weight, whatever its other numbers; a sum that is NaN
