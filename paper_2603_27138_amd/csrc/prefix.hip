@@ -228,7 +228,7 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(Pref
     }
     return e;
   };
-  UnitRegs<DT, DH> T;
+  UnitRegs<DT, DH> T;  // one unit in flight: two or three are no faster
   Entry e = entry(0, u0);
   issue_unit<DT, DH>(T, W.k_pool, W.v_pool, e, ln, kg);
   slots_next = fetch_slots(u0 + kWave * WAVES);
@@ -388,8 +388,8 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(Pref
 // ---- More rows than that, bf16: tiles of K and V through LDS.
 //
 // A group of WM waves has WM * 32 rows (each wave 32 of them) and goes through tiles of TOK tokens, each wave bringing TOK / WM of their rows
-// from memory into LDS, where all of the group read them.  WN groups take tiles in turn and fold their sums at the end.  Two tiles
-// lie in LDS: while one is multiplied the next one is on its way, without passing through registers.
+// from memory into LDS, where all of the group read them.  WN groups take tiles in turn and fold their sums at the end.  RING tiles
+// lie in LDS: while one is multiplied the next ones are on their way, without passing through registers.
 //   logits^T[token][row] = K . Q^T       32x32x16: K rows are the first operand (lane: token lane % 32, channels 8 * (lane / 32) + ..)
 //   out^T[channel][row] += V^T . P^T     32x32x16: the logits leave the first product with row lane % 32 and tokens 8 * (i / 4) + 4 * (lane / 32) +
 //                                        i % 4 in register i: eight registers are the second operand of a step of 16 tokens, if the
@@ -445,11 +445,12 @@ __global__ __launch_bounds__(WM* WN* kWave) void prefix_wide_kernel(PrefixPlan P
   constexpr int TILE = TOK * L::ROWB;                // bytes of K, and of V, of a tile
   constexpr int MINE = TILE / WM, NP = MINE / 1024;  // bytes and pieces of it that a wave brings
   constexpr int ROWS = TOK / WM;                     // token rows of it
+  constexpr int RING = 2;                            // (three ahead, where there is room: no faster)
   typedef std::conditional_t<(UNITS > 4), uint64_t, uint32_t> Counts;  // tokens that count of each unit of a tile, a byte for each
   static_assert(UNITS <= 8 && ROWS <= 16 && MINE % 1024 == 0, "a wave's rows are of one unit, in whole pieces");
   static_assert(STEP <= 32, "steps are cut from 64 units");
-  static_assert((WN - 1) * WM * (L::DT * 16 + 2) * 256 <= WN * 4 * TILE, "the groups' sums fit where the tiles were");
-  __shared__ __attribute__((aligned(1024))) char lds[WN * 4 * TILE];  // [group][tile at hand or next][K, V][tile]
+  static_assert((WN - 1) * WM * (L::DT * 16 + 2) * 256 <= WN * RING * 2 * TILE, "the groups' sums fit where the tiles were");
+  __shared__ __attribute__((aligned(1024))) char lds[WN * RING * 2 * TILE];  // [group][place][K, V][tile]
   __shared__ int2 queue[WM * WN][kWave];
   const PrefixItem it = P.item[blockIdx.x];  // in the trip that says whether it is one
   if (!made_for(P, stamp) || (int)blockIdx.x >= P.head[0]) return;
@@ -524,9 +525,9 @@ __global__ __launch_bounds__(WM* WN* kWave) void prefix_wide_kernel(PrefixPlan P
     v_from[i] = in * L::ROWB + ((c ^ L::v_swizzle(r)) << 4);
   }
   typedef __attribute__((address_space(3))) char* lds_ptr;
-  char* const mine = lds + grp * 4 * TILE;
+  char* const mine = lds + grp * RING * 2 * TILE;
   const uint32_t lds_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)mine + wm * MINE);
-  // The wave's part of the group's tile at u_pos, to place `to` (0 or 1).
+  // The wave's part of the group's tile at u_pos, to place `to`.
   auto request = [&](int to) __attribute__((always_inline)) {
     const int j = u_pos + grp * UNITS + row0 / 16;
     const int what = j < kWave ? __builtin_amdgcn_readlane(u_what, j & 63) : 0;
@@ -629,54 +630,50 @@ __global__ __launch_bounds__(WM* WN* kWave) void prefix_wide_kernel(PrefixPlan P
       }
   };
 
-  // The wave's part of the tile has arrived, so has everybody's behind the barrier, and nobody reads the tile before it any more.
-  auto arrive = [&]() __attribute__((always_inline)) {
-    await<0>();
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
-  refill();
-  if (u_n > 0) {
-    int at = 0;
-    bool full = is_full(), more;  // the step at hand is full; another one follows
-    Counts tokens = 0;            // of the group's tile in the step at hand, where that is not full
-    auto count = [&]() __attribute__((always_inline)) {
-      tokens = 0;
+  // Steps that are on their way, the one at hand among them; whether the last of them is not full, and the counts of the group's tile there.
+  int flying = 0, at = 0, next = 0;
+  bool partial = false;
+  Counts tokens = 0;
+  auto ask = [&]() __attribute__((always_inline)) {
+    if (u_n <= u_pos) return;
+    if (!is_full()) {
+      partial = true;
 #pragma unroll
       for (int u = 0; u < UNITS; ++u) {
         const int j = u_pos + grp * UNITS + u;
         tokens |= (Counts)(j < kWave ? __builtin_amdgcn_readlane(u_what, j & 63) & 255 : 0) << (8 * u);
       }
-    };
-    // The step at u_pos is on its way to place `at`; ask for the one behind it.
-    auto go_on = [&]() __attribute__((always_inline)) {
-      full = is_full();
-      if (!full) count();
-      u_pos += STEP;
-      if (u_n - u_pos < STEP) refill();
-      more = u_n > u_pos;
-    };
-    request(0);
-    go_on();
-    arrive();
-    if (more) request(1);
-    // full tiles: the branch to follow() is rare, and left out of the loop, where it would cost every tile copies of the sums
-    while (full) {
-      logits(mine + at * 2 * TILE);
-      float b = largest();
-      if (__ballot(b > m + kLag) != 0) follow(b);
-      values(mine + at * 2 * TILE + TILE);
-      if (!more) {
-        full = false;
-        tokens = 0;
-        break;
-      }
-      at ^= 1;
-      go_on();
-      arrive();
-      if (more) request(at ^ 1);
     }
-    if (tokens != 0) {  // the last step's tile is not full
+    request(next);
+    next = next == RING - 1 ? 0 : next + 1;
+    ++flying;
+    u_pos += STEP;
+    if (u_n - u_pos < STEP) refill();
+  };
+  // The wave's part of the step at hand has arrived, so has everybody's behind the barrier, and nobody reads the step before it any more.
+  auto arrive = [&]() __attribute__((always_inline)) {
+    if (flying == RING - 1) await<(RING - 2) * 2 * NP>();
+    else await<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  refill();
+#pragma unroll
+  for (int n = 0; n < RING - 1; ++n) ask();
+  // full tiles
+  while (flying > (int)partial) {
+    arrive();
+    ask();
+    logits(mine + at * 2 * TILE);
+    const float b = largest();
+    if (__ballot(b > m + kLag) != 0) follow(b);
+    values(mine + at * 2 * TILE + TILE);
+    at = at == RING - 1 ? 0 : at + 1;
+    --flying;
+  }
+  if (partial) {
+    arrive();
+    if (tokens != 0) {
       char* const v = mine + at * 2 * TILE + TILE;
       logits(mine + at * 2 * TILE);
 #pragma unroll
