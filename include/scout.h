@@ -526,8 +526,9 @@ int scout_prefix_plan(const scout_problem* p, int32_t n_prefix, int32_t prefix_b
  * A sequence without prefix and partial gives o = 0, m = -inf, l = 0, out = 0, lse = -inf.
  * m is the reference that l and o are relative to: the largest logit, or up to 16 ln 2 below it
  * (m + ln l is the same).
- * Products, sums and softmax weights are binary32; bf16 rounds the weights to bf16 before
- * the value product where only `out` is written, and to two bf16 terms (2^-16) where o is.
+ * Products, sums and softmax weights are binary32; with bf16 the weights enter the value
+ * product as two bf16 terms (2^-15), or as one (2^-8) where o is not written and a
+ * prefix has more than 64 rows (sequences times Hq / Hkv) on average.
  */
 int shared_prefix_attn(const scout_problem* p, int32_t n_prefix, int32_t prefix_blocks,
                        const void* plan, size_t plan_bytes, const void* q, const void* k_pool,

@@ -173,17 +173,22 @@ __device__ __forceinline__ int query_row(const PrefixPlan& P, const PrefixWork& 
   return P.member[it.member0 + (int)m] * W.Hq + it.head * W.G + (int)(rr - m * W.G);
 }
 
+// bf16 terms of a softmax weight in the second product (bf16 only).  Two: 2^-15 of a weight at the most is lost.  One, rounded, where the
+// result leaves as bf16 and the matrix instructions bound the pass: half a step, 2^-8 of each weight at the most, about as much as the output's
+// own rounding (2-norm against binary64: 1.65e-3 for that alone, 2.2e-3 with one term, 1.7e-3 with two).  Two terms instead of one cost 1 to 6 %
+// up to 64 rows, 20 % at 128, 34 % at 256.  The sum l always has the weights as they are.
+constexpr int kOneTermFrom = 128;  // rows of a tile
+
 constexpr int kNarrowWaves = 8;
 
-// Up to 64 rows.  The waves of a workgroup take units of 16 tokens in turn (wave v: v, v + 8, ...); K and V rows go from memory into
-// MFMA operand registers, and NQ column tiles of 16 rows are multiplied with them there (layout: see attn_unit.h).  Bound by memory: a unit is
-// 8 KiB at bf16, d = 128.  The waves fold through LDS.
-// TERMS: bf16 terms of a softmax weight in the second product (bf16 only).  One where the result leaves as bf16 (half a step of 2^-8 of each weight,
-// as much as the output's own rounding); two where it leaves in binary32 (2^-16).  The sum l always has the weights as they are.
-template <int DT, int DH, int NQ, int TERMS>
+// Up to 32 rows, and fp32.  The waves of a workgroup take units of 16 tokens in turn (wave v: v, v + 8, ...); K and V rows go from memory
+// into MFMA operand registers, and NQ column tiles of 16 rows are multiplied with them there (layout: see attn_unit.h).  The waves fold through LDS.
+// Bound by memory, and where there is little of it by a launch's way in and out: 4 sequences of 4 heads over 8192 shared tokens (8 KV heads,
+// 33.5 MB at bf16, d = 128) 8 us, of which 2.3 are the launch and 4 the way to the first unit and from the last; 2 of them over 65536 tokens 42 us (6.4 TB/s).
+template <int DT, int DH, int NQ>
 __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(PrefixPlan P, PrefixStamp stamp, PrefixWork W) {
   using L = Tile<DT, DH>;
-  constexpr int WAVES = kNarrowWaves, ROW = DH + 4;
+  constexpr int WAVES = kNarrowWaves, ROW = DH + 4, TERMS = 2;
   __shared__ float smem[WAVES * (16 * ROW + 32)];
   const PrefixItem it = P.item[blockIdx.x];  // in the trip that says whether it is one
   if (!made_for(P, stamp) || (int)blockIdx.x >= P.head[0]) return;
@@ -872,25 +877,26 @@ int launch_prefix_plan(const Dims& D, int dtype, int n_prefix, int prefix_blocks
   return hipGetLastError() == hipSuccess ? SCOUT_OK : SCOUT_EHIP;
 }
 
-template <int DT, int DH, int TERMS>
-static void launch_items(const PrefixShape& s, int grid, const PrefixPlan& P, const PrefixStamp& stamp, const PrefixWork& W, hipStream_t st) {
-  const dim3 g(grid);
-  if (s.tile_rows == 16) {
-    hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 1, TERMS>), g, dim3(512), 0, st, P, stamp, W);
-  } else if (s.tile_rows == 32) {
-    hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 2, TERMS>), g, dim3(512), 0, st, P, stamp, W);
-  } else if constexpr (DT == SCOUT_BF16) {
-    if (s.tile_rows == 64) hipLaunchKernelGGL((prefix_wide_kernel<DH, 2, 4, 32, TERMS>), g, dim3(512), 0, st, P, stamp, W);
-    else if (s.tile_rows == 128) hipLaunchKernelGGL((prefix_wide_kernel<DH, 4, 2, 64, TERMS>), g, dim3(512), 0, st, P, stamp, W);
-    else hipLaunchKernelGGL((prefix_wide_kernel<DH, 8, 1, 128, TERMS>), g, dim3(512), 0, st, P, stamp, W);
-  }
+template <int DH, int TERMS>
+static void launch_many_rows(const PrefixShape& s, int grid, const PrefixPlan& P, const PrefixStamp& stamp, const PrefixWork& W, hipStream_t st) {
+  if (s.tile_rows == 128) hipLaunchKernelGGL((prefix_wide_kernel<DH, 4, 2, 64, TERMS>), dim3(grid), dim3(512), 0, st, P, stamp, W);
+  else hipLaunchKernelGGL((prefix_wide_kernel<DH, 8, 1, 128, TERMS>), dim3(grid), dim3(512), 0, st, P, stamp, W);
 }
 
 template <int DT, int DH>
 static void launch_all(const Dims& D, const PrefixShape& s, int items, const PrefixPlan& P, const PrefixStamp& stamp, const PrefixWork& W,
                        const PrefixOut& E, hipStream_t st) {
-  if (DT == SCOUT_BF16 && E.o != nullptr) launch_items<DT, DH, 2>(s, items, P, stamp, W, st);
-  else launch_items<DT, DH, 1>(s, items, P, stamp, W, st);
+  const dim3 g(items);
+  if (s.tile_rows == 16) {
+    hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 1>), g, dim3(512), 0, st, P, stamp, W);
+  } else if (s.tile_rows == 32) {
+    hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 2>), g, dim3(512), 0, st, P, stamp, W);
+  } else if constexpr (DT == SCOUT_BF16) {
+    static_assert(kOneTermFrom == 128, "below, two");
+    if (s.tile_rows == 64) hipLaunchKernelGGL((prefix_wide_kernel<DH, 2, 4, 32, 2>), g, dim3(512), 0, st, P, stamp, W);
+    else if (E.o != nullptr) launch_many_rows<DH, 2>(s, items, P, stamp, W, st);
+    else launch_many_rows<DH, 1>(s, items, P, stamp, W, st);
+  }
   hipLaunchKernelGGL((prefix_combine_kernel<DT, DH>), dim3((D.B * D.Hq + 3) / 4), dim3(256), 0, st, P, stamp, W, E);
 }
 
