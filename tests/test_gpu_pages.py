@@ -336,3 +336,81 @@ def test_captured_steps():
             assert torch.equal(eager[key], captured[key]), (turn, key)
         assert torch.equal(eager["pages"][:80], captured["pages"][:80])
     assert eager["status"].tolist() == [0] * n and eager["short"].item() == 0
+
+
+def test_tiles_beyond_four_gib():
+    """Slots whose tiles lie beyond 4 GiB of a pool: copied by a deep fork, moved by a compaction."""
+    S, d, Hkv, n_slots = 64, 128, 1, 150_000   # 32 KiB a tile: 4.9 GB a pool
+    i32 = dict(dtype=torch.int32, device="cuda")
+    k, v = (torch.zeros(n_slots, S, d, device="cuda") for _ in range(2))
+    table, ctx = torch.full((3, Hkv, 4), -1, **i32), torch.tensor([4 * S, -1, -1], **i32)
+    far = torch.tensor([n_slots - 1, n_slots - 7, 140_000, 139_999], **i32)
+    table[0, 0] = far
+    tiles = [torch.randn(4, S, d, device="cuda") for _ in range(2)]
+    for pool, t in zip((k, v), tiles):
+        pool[far.long()] = t
+    digest = torch.zeros(3, Hkv, 4, 2, d, device="cuda")
+    p = B.make_problem(3, 1, Hkv, d, S, B.F32, 4, 1, ctx)
+    pages = B.alloc_pages(n_slots)
+    B.pages_init(p, ctx, table, n_slots, pages)
+    held = pages[:n_slots].clone()
+    filler = torch.full((1, 1, n_slots), -1, **i32)   # everything but the last slots is somebody's
+    filler[0, 0, :n_slots - 20] = torch.arange(n_slots - 20, **i32)
+    words = -(-n_slots // 64) * 64
+    pages[:n_slots - 20] += 1
+    pages[words:words + (n_slots - 20) // 32] = -1
+    status = torch.empty(1, **i32)
+    B.fork_sequences(p, torch.tensor([0], **i32), torch.tensor([1], **i32), True, ctx, digest, table, k, v, n_slots, pages, status)
+    assert status.item() == 0 and int(table[1].min()) >= 149_900
+    for pool, t in zip((k, v), tiles):
+        assert torch.equal(pool[table[1, 0].long()], t)
+    pages[:n_slots] = held
+    pages[:n_slots].index_add_(0, table[1, 0].long(), torch.ones(4, **i32))
+    bits = (pages[:n_slots] > 0).cpu().numpy().astype(np.uint8)
+    bits = np.concatenate([bits, np.zeros(-len(bits) % 32, np.uint8)])
+    pages[words:words + len(bits) // 32] = torch.from_numpy(np.packbits(bits.reshape(-1, 32), axis=1, bitorder="little").view(np.int32).ravel().copy()).cuda()
+    slot_map, live = torch.empty(n_slots, **i32), torch.empty(1, **i32)
+    B.compact_pool(p, table, k, v, n_slots, pages, slot_map, live)
+    assert live.item() == 8 and int(table.max()) == 7
+    for pool, t in zip((k, v), tiles):
+        assert torch.equal(pool[table[0, 0].long()], t) and torch.equal(pool[table[1, 0].long()], t)
+
+
+def test_neighbours_are_left_alone():
+    """What lies around the outputs stays as it is."""
+    rng = np.random.default_rng(14)
+    c = Cache(rng, 5, 2, 16, 64, torch.bfloat16, 3, 37, [40, 33, -1, -1, 16], share=1.0)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    guard = lambda n: torch.full((n + 32,), 0x5a5a5a5a, **i32)  # noqa: E731
+    bufs = {name: guard(n) for name, n in dict(status=2, new=10, short=1, where=37, live=1).items()}
+    of = lambda name, n: bufs[name][16:16 + n]  # noqa: E731
+    B.fork_sequences(c.p, torch.tensor([0, 1], **i32), torch.tensor([2, 3], **i32), False, *c.cache(), of("status", 2))
+    B.reserve_blocks(c.p, c.ctx, c.n_slots, c.pages, of("new", 10), of("short", 1))
+    B.compact_pool(c.p, c.table, c.k_pool, c.v_pool, c.n_slots, c.pages, of("where", 37), of("live", 1))
+    torch.cuda.synchronize()
+    for name, b in bufs.items():
+        n = b.numel() - 32
+        assert bool((b[:16] == 0x5a5a5a5a).all()) and bool((b[16 + n:] == 0x5a5a5a5a).all()), name
+        assert not bool((b[16:16 + n] == 0x5a5a5a5a).any()), name
+
+
+def test_both_marshallers_pass_the_same():
+    """Recorded calls (ctypes) leave what the calls themselves leave (the extension module)."""
+    states = []
+    for recorded in (False, True):
+        rng = np.random.default_rng(15)
+        c = Cache(rng, 6, 2, 16, 64, torch.bfloat16, 4, 60, [50, 32, -1, -1, -1, 20], share=1.0)
+        i32 = dict(dtype=torch.int32, device="cuda")
+        keep = dict(src=torch.tensor([0, 1], **i32), dst=torch.tensor([2, 3], **i32), gone=torch.tensor([0, 5], **i32),
+                    status=torch.empty(2, **i32), new=torch.empty(6, 2, **i32), short=torch.empty(1, **i32), where=torch.empty(60, **i32),
+                    live=torch.empty(1, **i32))
+        calls = [(B.pages_init, (c.p, c.ctx, c.table, 60, c.pages)),
+                 (B.fork_sequences, (c.p, keep["src"], keep["dst"], True, *c.cache(), keep["status"])),
+                 (B.free_sequences, (c.p, keep["gone"], c.ctx, c.table, 60, c.pages)),
+                 (B.compact_pool, (c.p, c.table, c.k_pool, c.v_pool, 60, c.pages, keep["where"], keep["live"])),
+                 (B.reserve_blocks, (c.p, c.ctx, 60, c.pages, keep["new"], keep["short"]))]
+        for fn, args in calls:
+            B.prepare(fn, *args)() if recorded else fn(*args)
+        torch.cuda.synchronize()
+        states.append([c.ctx, c.table, c.digest, c.k_pool, c.v_pool, c.pages[:60], *list(keep.values())])
+    assert all(torch.equal(x, y) for x, y in zip(*states))

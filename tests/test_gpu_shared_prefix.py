@@ -364,3 +364,60 @@ def test_both_marshallers_pass_the_same():
         c()
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(eager, (b.out, b.lse, b.o, b.m, b.l)))
+
+
+def test_graphs_that_share_a_workspace():
+    """Two captured batches with one workspace, replayed in turn."""
+    a, c = (Batch(s, BF16, 128, 32, 8, 2, [1500, 40], _of(2, 14), other=False) for s in (19, 20))
+    a.run().check()
+    c.run().check()
+    want = [(x.out.clone(), x.lse.clone()) for x in (a, c)]
+    ws = a.ws
+    graphs, keep = [], []
+    for x in (a, c):
+        q, table, graph = x.q.cuda(), x.table.cuda(), torch.cuda.CUDAGraph()
+        keep.append((q, table))
+        with torch.cuda.graph(graph):
+            B.shared_prefix_attn(x.p, 2, x.blocks, x.plan, q, x.k_dev, x.v_dev, x.n_slots, table, None, None, None, None, None, None, x.out, x.lse, ws)
+        graphs.append(graph)
+    for turn in range(4):
+        for x in (a, c):
+            x.out.zero_(), x.lse.zero_()
+        for g in graphs if turn % 2 else graphs[::-1]:
+            g.replay()
+        torch.cuda.synchronize()
+        for x, (out, lse) in zip((a, c), want):
+            assert torch.equal(x.out, out) and torch.equal(x.lse, lse), turn
+
+
+@pytest.mark.parametrize("n", [3, 30])
+def test_neighbours_are_left_alone(n):
+    b = Batch(21, BF16, 64, 16, 4, 1, [130, 17], _of(2, n), other=False)
+    sizes = dict(out=n * 4 * 64, lse=n * 4, o=n * 4 * 64, m=n * 4, l=n * 4)
+    bufs = {k: torch.full((v + 128,), 7.0, dtype=b.dtype if k == "out" else F32, device="cuda") for k, v in sizes.items()}
+    at = {k: bufs[k][64:64 + v] for k, v in sizes.items()}
+    plan = torch.full((b.plan.numel() + 1024,), 0x5a, dtype=torch.uint8, device="cuda")
+    inner = plan[512:512 + b.plan.numel()]
+    B.prefix_plan(b.p, 2, b.blocks, b.of_dev, b.len_dev, inner)
+    B.shared_prefix_attn(b.p, 2, b.blocks, inner, b.q.cuda(), b.k_dev, b.v_dev, b.n_slots, b.table.cuda(), None, None, None, at["o"], at["m"],
+                         at["l"], at["out"], at["lse"], b.ws)
+    torch.cuda.synchronize()
+    b.out, b.lse, b.o, b.m, b.l = (at[k].view(n, 4, -1).squeeze(-1) if sizes[k] == n * 4 else at[k].view(n, 4, 64) for k in ("out", "lse", "o", "m", "l"))
+    b.check()
+    for k, v in sizes.items():
+        assert bool((bufs[k][:64] == 7.0).all()) and bool((bufs[k][64 + v:] == 7.0).all()), k
+    assert bool((plan[:512] == 0x5a).all()) and bool((plan[512 + b.plan.numel():] == 0x5a).all())
+
+
+def test_many_prefixes():
+    """As many as a plan takes, most of them nobody's."""
+    P, n = 2048, 70
+    lens = [(7 * i) % 45 for i in range(P)]
+    Batch(22, BF16, 64, 16, 2, 1, lens, [(29 * b) % P for b in range(n)], other=False).run().check()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_long_prefix_in_many_splits(dtype):
+    """Windows of units, and of a wave's list entries, one after the other; blocks without a slot in between."""
+    for n, G in ((1, 2), (20, 8)):
+        Batch(23, dtype, 64, 16, G, 1, [70_003], [0] * n, p_host=0.4, other=False).run().check()
