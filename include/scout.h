@@ -435,7 +435,8 @@ int scout_pages_init(const scout_problem* p, const int32_t* ctx_len, int32_t* bl
  * lowest free slot, in the order of the pairs.  The others, and takers for whom none
  * is left (then the caller keeps the block on the host, as append_token has it), get -1.
  * A reserved slot counts as held from here on; the append that follows puts it into
- * the table.
+ * the table.  Until then no row names it: reserve once for an append, and free or fork
+ * onto a sequence only behind it, or the slot stays held.
  *   new_slot  i32 [B][Hkv]  out: append_token's argument
  *   n_short   i32 [1]       out: takers for whom no slot was left
  */
@@ -455,7 +456,8 @@ int reserve_blocks(const scout_problem* p, const int32_t* ctx_len, int64_t n_slo
  * host copies are the caller's to make).
  * A fork is refused, and changes nothing, if src[i] or dst[i] is outside [0, B),
  * dst[i] holds tokens (ctx_len > 0: free it first), is src of any fork of the call or
- * dst of an earlier one.
+ * dst of an earlier one.  dst[i]'s row must name no slot, as it does once the sequence
+ * is freed: what it names is overwritten and stays held.
  *   src, dst  i32 [n], n <= B  DEVICE
  *   digest, block_table, k_pool, v_pool, ctx_len   in/out, as in append_token
  *   status    i32 [n]  out: -1 refused; else the number of blocks for which no slot was left

@@ -11,39 +11,11 @@
 // table rows, tiles).
 #include "pages.h"
 
+#include "plan_scan.h"
+
 namespace scout {
 
-constexpr int kPlanThreads = 1024;
-constexpr int kPlanWaves = kPlanThreads / kWave;
 constexpr int kCopyThreads = 256;
-
-// Inclusive sum over the lanes of a wave.
-__device__ __forceinline__ int wave_scan(int x, int lane) {
-#pragma unroll
-  for (int s = 1; s < kWave; s <<= 1) {
-    const int y = __shfl_up(x, s);
-    if (lane >= s) x += y;
-  }
-  return x;
-}
-
-// Exclusive sum over the threads of the planning workgroup, and the total; `lds`: kPlanWaves words.
-__device__ __forceinline__ int plan_scan(int x, int* lds, int* total) {
-  const int lane = lane_id(), wave = threadIdx.x / kWave;
-  const int inc = wave_scan(x, lane);
-  __syncthreads();  // the words may still be read from the call before
-  if (lane == kWave - 1) lds[wave] = inc;
-  __syncthreads();
-  int before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kPlanWaves; ++w) {
-    const int t = lds[w];
-    before += w < wave ? t : 0;
-    all += t;
-  }
-  *total = all;
-  return before + inc - x;
-}
 
 // Bits of slots that exist, of word w.
 __device__ __forceinline__ uint32_t exists(long long n_slots, long long w) {
@@ -285,7 +257,7 @@ constexpr int kForkBatch = 4;                 // children that a workgroup write
 // of a KV head (shallow: the last block; deep: a range), for as many.  What the children of one parent take is read once.
 __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P, int n, const int32_t* __restrict__ dst, int deep,
                                                                  int32_t* ctx_len, char* digest, int entry_bytes, int32_t* table,
-                                                                 char* k_pool, char* v_pool, int tile_bytes, int stride_bytes,
+                                                                 char* k_pool, char* v_pool, int tile_bytes, long long stride_bytes,
                                                                  int row_wgs, int row_blocks, int row_parts, int parts, int entries) {
   const bool rows = (int)blockIdx.x < row_wgs;
   const int w = rows ? blockIdx.x : blockIdx.x - row_wgs;
@@ -497,7 +469,7 @@ __device__ __forceinline__ int slot_after(const Pages& P, int slot, int n_live, 
 }
 
 __global__ __launch_bounds__(kCopyThreads) void compact_move_kernel(Pages P, int move_wgs, int map_wgs, long long entries, int32_t* table,
-                                                                    char* k_pool, char* v_pool, int tile_bytes, int stride_bytes,
+                                                                    char* k_pool, char* v_pool, int tile_bytes, long long stride_bytes,
                                                                     int32_t* slot_map) {
   const int n_live = P.head[0], moves = P.head[1], above_from = P.head[2];
   int w = blockIdx.x;
@@ -559,8 +531,6 @@ int launch_fork(const Dims& D, int dtype, const Pages& P, int n, const int32_t* 
   if (n == 0) return SCOUT_OK;
   const int es = dtype == SCOUT_BF16 ? 2 : 4;
   const int entry_bytes = D.digest_kind == 1 ? D.d * 4 : 2 * D.d * es, tile_bytes = D.S * D.d * es;
-  if (deep) hipLaunchKernelGGL(fork_count_kernel, dim3(n * D.Hkv), dim3(kCopyThreads), 0, st, D, P, src, ctx_len, table);
-  hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, D, P, n, src, dst, deep, ctx_len, table, status);
   const int row_blocks = kRowPieces * 16 / entry_bytes;  // 8 to 32
   const long long pairs = (long long)(n + kForkBatch - 1) / kForkBatch * D.Hkv;
   const int row_parts = (D.max_blocks + row_blocks - 1) / row_blocks;
@@ -569,9 +539,12 @@ int launch_fork(const Dims& D, int dtype, const Pages& P, int n, const int32_t* 
   // time (2 heads of 65 blocks: 5.3 us for the launch, 8.6 with four), else four, which share the way to their first tile.
   const int entries = pairs * D.max_blocks <= 2048 ? 1 : 4;
   const int parts = deep ? (D.max_blocks + entries - 1) / entries : 1;
+  if ((row_wgs + pairs * parts) * kCopyThreads >= 1ll << 32) return SCOUT_EUNSUPPORTED;  // threads of a launch
+  if (deep) hipLaunchKernelGGL(fork_count_kernel, dim3(n * D.Hkv), dim3(kCopyThreads), 0, st, D, P, src, ctx_len, table);
+  hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, D, P, n, src, dst, deep, ctx_len, table, status);
   hipLaunchKernelGGL(fork_copy_kernel, dim3((unsigned)(row_wgs + pairs * parts)), dim3(kCopyThreads), 0, st, D, P, n, dst, deep, ctx_len,
                      static_cast<char*>(digest), entry_bytes, table, static_cast<char*>(k_pool), static_cast<char*>(v_pool), tile_bytes,
-                     D.tile_stride * es, (int)row_wgs, row_blocks, row_parts, parts, entries);
+                     (long long)D.tile_stride * es, (int)row_wgs, row_blocks, row_parts, parts, entries);
   return launched();
 }
 
@@ -591,8 +564,8 @@ int launch_compact(const Dims& D, int dtype, const Pages& P, int32_t* table, voi
   const long long half = (P.n_slots + 1) / 2;  // at most so many tiles can move
   const int move_wgs = (int)(half < 1 ? 1 : half > 2048 ? 2048 : half), map_wgs = (int)wgs_for(P.n_slots, 512);
   hipLaunchKernelGGL(compact_move_kernel, dim3(move_wgs + map_wgs + wgs_for(entries, 1024)), dim3(kCopyThreads), 0, st, P, move_wgs,
-                     map_wgs, entries, table, static_cast<char*>(k_pool), static_cast<char*>(v_pool), D.S * D.d * es, D.tile_stride * es,
-                     slot_map);
+                     map_wgs, entries, table, static_cast<char*>(k_pool), static_cast<char*>(v_pool), D.S * D.d * es,
+                     (long long)D.tile_stride * es, slot_map);
   return launched();
 }
 

@@ -11,6 +11,7 @@
 #include <type_traits>
 
 #include "attn_unit.h"
+#include "plan_scan.h"
 #include "prefix.h"
 
 namespace scout {
@@ -18,8 +19,6 @@ namespace scout {
 typedef __attribute__((ext_vector_type(8))) short s16x8;
 
 // ---------------------------------------------------------------- the plan
-
-constexpr int kPlanThreads = 1024;
 
 struct PrefixStamp {
   int32_t w[PrefixPlan::kStampWords];
@@ -34,15 +33,16 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PrefixPlan P,
                                                                    const int32_t* __restrict__ prefix_of,
                                                                    const int32_t* __restrict__ prefix_len) {
   // of each prefix: its sequences, how many of them have been put in the list, where its part of the list starts, its tokens, its
-  // first item
-  __shared__ int count[kMaxPrefixes], placed[kMaxPrefixes], first[kMaxPrefixes], len[kMaxPrefixes], base[kMaxPrefixes + 1];
-  __shared__ int chunk_lds, longest_lds, best_lds;
-  const int t = threadIdx.x;
+  // tiles of rows (of all KV heads), its first item
+  __shared__ int count[kMaxPrefixes], placed[kMaxPrefixes], first[kMaxPrefixes], len[kMaxPrefixes], tiles[kMaxPrefixes], base[kMaxPrefixes];
+  __shared__ int lds[kPlanWaves], items_lds[kWave], longest_lds, chunk_lds;
+  const int t = threadIdx.x, lane = lane_id();
   for (int p = t; p < n_prefix; p += kPlanThreads) {
     const int n = prefix_len[p];
     len[p] = n < 0 ? 0 : n > max_tokens ? max_tokens : n;
     count[p] = placed[p] = 0;
   }
+  if (t < kWave) items_lds[t] = 0;
   if (t == 0) longest_lds = 0;
   __syncthreads();
   for (int b = t; b < B; b += kPlanThreads) {
@@ -50,34 +50,17 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PrefixPlan P,
     if (p >= 0 && p < n_prefix) atomicAdd(&count[p], 1);
   }
   __syncthreads();
-  for (int p = t; p < n_prefix; p += kPlanThreads) {
-    if (count[p] == 0) len[p] = 0;  // nobody has it
-    atomicMax(&longest_lds, len[p]);
-  }
-  if (t == 0) {
-    int at = 0;
-    for (int p = 0; p < n_prefix; ++p) {
-      first[p] = at;
-      at += count[p];
-    }
-  }
-  __syncthreads();
-  const int longest = longest_lds;
-  auto tiles_of = [&](int p) { return (int)(((long long)count[p] * G + shape.tile_rows - 1) / shape.tile_rows); };
   // How long a chunk is: candidate c cuts the longest prefix c + 1 ways.  shape.slots workgroups run at a time, so a candidate costs as
   // many rounds as its items fill, each as long as a chunk and what an item costs beyond its tokens.
-  auto chunk_of = [&](int c) {
+  static_assert(kMaxPrefixSplits == kWave, "a candidate, and a split, per lane");
+  auto chunk_of = [&](int longest, int c) {
     const int n = round_up((longest + c) / (c + 1), shape.granule);
     return n > shape.granule ? n : shape.granule;
   };
-  static_assert(kMaxPrefixSplits == kWave, "a candidate, and a split, per lane");
-  if (t < kWave) {
-    const int c = chunk_of(t);
-    long long items = 0;
-    for (int p = 0; p < n_prefix; ++p) items += (long long)tiles_of(p) * Hkv * splits_of(len[p], c);
+  auto cheapest = [&](int items, int chunk) {  // by a wave, lane c with candidate c's items (below kMostItems * kMaxPrefixSplits) and chunk
     const long long rounds = (items + shape.slots - 1) / shape.slots;
-    long long cost = items > P.max_items ? 1ll << 62 : rounds * (c + shape.head_cost);  // without splits the items always fit
-    int best = t;
+    long long cost = items > P.max_items ? 1ll << 62 : rounds * (chunk + shape.head_cost);  // without splits the items always fit
+    int best = lane;
 #pragma unroll
     for (int s = 1; s < kWave; s <<= 1) {  // the lowest cost, of equal ones the fewest splits
       const long long other = __shfl_xor(cost, s);
@@ -87,24 +70,71 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PrefixPlan P,
         best = who;
       }
     }
-    if (t == 0) best_lds = best;
-  }
-  __syncthreads();
-  if (t == 0) {
-    const int best = best_lds;
-    const int chunk = chunk_of(best);
-    int at = 0;
-    for (int p = 0; p < n_prefix; ++p) {
-      base[p] = at;
-      at += tiles_of(p) * Hkv * splits_of(len[p], chunk);
+    return __shfl(chunk, best);
+  };
+  auto tiles_for = [&](int members) { return (members * G + shape.tile_rows - 1) / shape.tile_rows * Hkv; };
+  int chunk, n_items = 0;
+  if (n_prefix <= kWave) {  // a wave has a prefix in each lane, and need not wait for the others (4 prefixes: 5 us with the launch, 6 below)
+    if (t < kWave) {
+      const int members = lane < n_prefix ? count[lane] : 0, my_tiles = tiles_for(members), my_len = members > 0 ? len[lane] : 0;
+      int longest = my_len, items = 0;
+#pragma unroll
+      for (int s = 1; s < kWave; s <<= 1) longest = max(longest, __shfl_xor(longest, s));
+      const int my_chunk = chunk_of(longest, lane);
+      for (int p = 0; p < n_prefix; ++p)
+        items += __builtin_amdgcn_readlane(my_tiles, p) * splits_of(__builtin_amdgcn_readlane(my_len, p), my_chunk);
+      const int best = cheapest(items, my_chunk), my_items = my_tiles * splits_of(my_len, best);
+      const int behind = wave_scan(members, lane), items_behind = wave_scan(my_items, lane);
+      if (lane < n_prefix) {
+        first[lane] = behind - members;
+        tiles[lane] = my_tiles;
+        len[lane] = my_len;
+        base[lane] = items_behind - my_items;
+      }
+      if (lane == kWave - 1) {
+        chunk_lds = best;
+        items_lds[0] = items_behind;
+      }
     }
-    base[n_prefix] = at;
-    chunk_lds = chunk;
-    P.head[0] = at;
+    __syncthreads();
+    chunk = chunk_lds;
+    n_items = items_lds[0];
+  } else {
+    for (int p0 = 0, at = 0; p0 < n_prefix; p0 += kPlanThreads) {
+      const int p = p0 + t, members = p < n_prefix ? count[p] : 0;
+      int total;
+      const int before = plan_scan(members, lds, &total);
+      if (p < n_prefix) {
+        first[p] = at + before;
+        tiles[p] = tiles_for(members);
+        if (members == 0) len[p] = 0;  // nobody has it
+        atomicMax(&longest_lds, len[p]);
+      }
+      at += total;
+    }
+    __syncthreads();
+    const int my_chunk = chunk_of(longest_lds, lane);
+    int items = 0;  // of the wave's prefixes
+    for (int p = t / kWave; p < n_prefix; p += kPlanWaves) items += tiles[p] * splits_of(len[p], my_chunk);
+    if (items > 0) atomicAdd(&items_lds[lane], items);
+    __syncthreads();
+    if (t < kWave) {
+      const int best = cheapest(items_lds[lane], my_chunk);
+      if (t == 0) chunk_lds = best;
+    }
+    __syncthreads();
+    chunk = chunk_lds;
+    for (int p0 = 0; p0 < n_prefix; p0 += kPlanThreads) {
+      const int p = p0 + t;
+      int total;
+      const int before = plan_scan(p < n_prefix ? tiles[p] * splits_of(len[p], chunk) : 0, lds, &total);
+      if (p < n_prefix) base[p] = n_items + before;
+      n_items += total;
+    }
+    __syncthreads();
   }
+  if (t == 0) P.head[0] = n_items;
   if (t < PrefixPlan::kStampWords) P.stamp[t] = stamp.w[t];
-  __syncthreads();
-  const int chunk = chunk_lds;
   for (int b = t; b < B; b += kPlanThreads) {
     const int p = prefix_of[b];
     const bool has = p >= 0 && p < n_prefix;
@@ -112,21 +142,21 @@ __global__ __launch_bounds__(kPlanThreads) void prefix_plan_kernel(PrefixPlan P,
     // in whichever order the additions come: a row's result does not depend on the rows beside it
     if (has) P.member[first[p] + atomicAdd(&placed[p], 1)] = b;
   }
-  for (int i = t; i < base[n_prefix]; i += kPlanThreads) {
+  for (int i = t; i < n_items; i += kPlanThreads) {
     int p = 0, hi = n_prefix - 1;  // the last prefix whose items start at i or before: the one that i belongs to
     while (p < hi) {
       const int mid = (p + hi + 1) >> 1;
       if (base[mid] <= i) p = mid;
       else hi = mid - 1;
     }
-    const int s = splits_of(len[p], chunk), units = Hkv * s, tiles = tiles_of(p);
+    const int s = splits_of(len[p], chunk), units = Hkv * s, of = tiles[p] / Hkv;  // tiles of rows of a unit
     // A unit (split, KV head) has a workgroup per tile of rows, and all of them read the same tokens: their numbers are eight apart,
     // so that they run on the same XCD and find in its L2 what one of them has read.
-    const int k = i - base[p], full = units / 8 * 8 * tiles;
+    const int k = i - base[p], full = units / 8 * 8 * of;
     int unit, tile;
     if (k < full) {
-      unit = k / (8 * tiles) * 8 + k % 8;
-      tile = k / 8 % tiles;
+      unit = k / (8 * of) * 8 + k % 8;
+      tile = k / 8 % of;
     } else {
       unit = units / 8 * 8 + (k - full) % (units % 8);
       tile = (k - full) / (units % 8);
@@ -852,10 +882,13 @@ static PrefixShape prefix_shape(const Dims& D, int dtype, int n_prefix) {
   return s;
 }
 
+// Items are workgroups of 512 threads, of which a launch has below 2^32.
+constexpr long long kMostItems = 1ll << 23;
+
 static int max_items(const Dims& D, const PrefixShape& s, int n_prefix) {
   const long long tiles = (long long)D.B * D.G / s.tile_rows + n_prefix;
   const long long n = tiles * D.Hkv + 2 * s.slots;
-  return n > (1 << 28) ? -1 : (int)n;
+  return n >= kMostItems ? -1 : (int)n;
 }
 
 static PrefixStamp prefix_stamp(const Dims& D, int dtype, const PrefixShape& s, int n_prefix, int prefix_blocks, int items) {

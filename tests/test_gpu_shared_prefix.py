@@ -421,3 +421,10 @@ def test_a_long_prefix_in_many_splits(dtype):
     """Windows of units, and of a wave's list entries, one after the other; blocks without a slot in between."""
     for n, G in ((1, 2), (20, 8)):
         Batch(23, dtype, 64, 16, G, 1, [70_003], [0] * n, p_host=0.4, other=False).run().check()
+
+
+def test_many_prefixes_that_somebody_has():
+    """More prefixes than the planning workgroup has threads, more sequences than that too."""
+    P, n = 1500, 1700
+    lens = [(13 * i) % 37 for i in range(P)]
+    Batch(24, BF16, 64, 16, 1, 1, lens, [(11 * b) % P if b % 5 else -1 for b in range(n)], other=False).run().check()

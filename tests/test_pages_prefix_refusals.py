@@ -75,6 +75,17 @@ def test_bad_arguments(name, kw, code):
     assert _call(name, _problem(), **kw) == code
 
 
+@pytest.mark.parametrize("name,problem,kw", [
+    # more workgroups than a launch can have
+    ("fork_sequences", dict(B=65535, Hq=1, Hkv=1, max_blocks=16384), dict(n=65535, deep=1)),
+    ("fork_sequences", dict(B=65535, Hq=1, Hkv=1, max_blocks=16384), dict(n=65535, deep=0)),
+    ("scout_prefix_plan", dict(B=1, Hq=8192, Hkv=8192), dict(n_prefix=2048)),
+    ("shared_prefix_attn", dict(B=1, Hq=8192, Hkv=8192), dict(n_prefix=2048)),
+])
+def test_more_than_a_launch_holds(name, problem, kw):
+    assert _call(name, _problem(**problem), **kw) == -2
+
+
 def test_sizes():
     n = ctypes.c_size_t(0)
     L = B.lib()
