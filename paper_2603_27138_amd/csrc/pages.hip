@@ -23,33 +23,54 @@ __device__ __forceinline__ uint32_t exists(long long n_slots, long long w) {
   return left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
 }
 
+// Words of `used` that slots are taken from, put in a row so that all waves hand them out: few takers find their slots in few
+// words, many in all of them.
+struct TakenWords {
+  int n[2];  // by turns, so that one can be cleared while the other is read
+  uint32_t bits[kPlanThreads];
+  int word[kPlanThreads], rank[kPlanThreads];
+};
+
 // The `want` lowest free slots, ascending, to list (as many as there are; the number is returned to every thread).  They
 // become used with one reference each.  The whole planning workgroup calls this.
 __device__ int take_lowest(const Pages& P, long long want, int32_t* list, int* lds) {
+  __shared__ TakenWords T;
   const long long nw = words_of(P.n_slots);
   const int lane = lane_id();
   long long got = 0;
-  for (long long w0 = 0; w0 < nw && got < want; w0 += kPlanThreads) {
+  int turn = 0;
+  if (threadIdx.x < 2) T.n[threadIdx.x] = 0;
+  for (long long w0 = 0; w0 < nw && got < want; w0 += kPlanThreads, turn ^= 1) {
     const long long w = w0 + threadIdx.x;
-    uint32_t free_bits = 0;
-    if (w < nw) free_bits = ~P.used[w] & exists(P.n_slots, w);
+    const uint32_t old = w < nw ? P.used[w] : ~0u, free_bits = ~old & exists(P.n_slots, w);
     int total;
     const long long at = got + plan_scan(__popc(free_bits), lds, &total);
+    if (threadIdx.x == 0) T.n[turn ^ 1] = 0;
     uint32_t taken = at < want ? free_bits : 0u;
     for (long long more = taken ? at + __popc(taken) - want : 0; more > 0; --more) taken &= ~(0x80000000u >> __clz(taken));  // the highest ones stay
-    if (taken) P.used[w] |= taken;
-    // Two words of the wave at a time, a lane per slot, so that neighbours are stored together (a word per lane: five times as long).
-    if (__ballot(taken != 0) != 0) {
-#pragma unroll 4
-      for (int k = 0; k < kWave; k += 2) {
-        const int from = k + lane / 32;
-        const uint32_t bits = __shfl(taken, from), bit = 1u << (lane & 31);
-        const int first = __shfl((int)at, from);
-        if (bits & bit) {
-          const int slot = (int)((w0 + (threadIdx.x - lane) + from) * 32) + (lane & 31);
-          list[first + __popc(bits & (bit - 1))] = slot;
-          P.refs[slot] = 1;
-        }
+    const uint64_t takes = __ballot(taken != 0);
+    if (takes != 0) {
+      int first = 0;
+      if (lane == 0) first = atomicAdd(&T.n[turn], (int)__popcll(takes));
+      first = __builtin_amdgcn_readfirstlane(first);
+      if (taken) {
+        P.used[w] = old | taken;
+        const int to = first + mbcnt64(takes);
+        T.bits[to] = taken;
+        T.word[to] = (int)w;
+        T.rank[to] = (int)at;
+      }
+    }
+    __syncthreads();
+    // two words of a wave at a time, a lane per slot, so that neighbours are stored together
+    const int n = T.n[turn];
+#pragma unroll 2
+    for (int k = threadIdx.x / 32; k < n; k += kPlanThreads / 32) {
+      const uint32_t bits = T.bits[k], bit = 1u << (lane & 31);
+      if (bits & bit) {
+        const int slot = T.word[k] * 32 + (lane & 31);
+        list[T.rank[k] + __popc(bits & (bit - 1))] = slot;
+        P.refs[slot] = 1;
       }
     }
     got += total;
