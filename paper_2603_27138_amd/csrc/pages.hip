@@ -275,12 +275,12 @@ struct TilePart {
 constexpr int kPartBytes = kTilePieces * kCopyThreads * 16;
 
 constexpr int kRowPieces = 2 * kCopyThreads;  // 16-byte pieces of digests that a workgroup holds at a time
-constexpr int kForkBatch = 4;                 // children that a workgroup writes to
+constexpr int kRowBatch = 4, kTileBatch = 2;  // children that a workgroup writes digests, and tiles, to
 
-// The first row_wgs workgroups: digests and table entries of a range of blocks of a KV head, for kForkBatch children.  The others: tiles
-// of a KV head (shallow: the last block; deep: a range), for as many.  What the children of one parent take is read once.  Bound by what is
-// written: 16 children of 32k tokens, 67 MB of digests: 15.4 us (4.4 TB/s); 48 of four parents, 172 MB: 34 us (5.1 TB/s); four deep ones,
-// 269 MB of tiles: 84 us, with the 67 MB that are read once 4.0 TB/s; the tiles lie as the pool's order has them, 8 KiB at a time.
+// The first row_wgs workgroups: digests and table entries of a range of blocks of a KV head, for kRowBatch children.  The others: tiles
+// of a KV head (shallow: the last block; deep: a range), for kTileBatch.  What the children of one parent take is read once for as many of them.
+// Bound by what is written: 16 children of 32k tokens, 67 MB of digests: 15.4 us (4.4 TB/s; two at a time: 15.6); 48 of four parents, 172 MB:
+// 34 us (5.1 TB/s; two at a time: 38); four deep ones, 269 MB of tiles: 64 us (4.2 TB/s, 5.2 with what is read; four at a time 78, one 86).
 __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P, int n, const int32_t* __restrict__ dst, int deep,
                                                                  int32_t* ctx_len, char* digest, int entry_bytes, int32_t* table,
                                                                  char* k_pool, char* v_pool, int tile_bytes, long long stride_bytes,
@@ -288,11 +288,12 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P
   const bool rows = (int)blockIdx.x < row_wgs;
   const int w = rows ? blockIdx.x : blockIdx.x - row_wgs;
   const int of = rows ? row_parts : parts, part = w % of, g = w / of % D.Hkv, batch = w / of / D.Hkv;
-  const int i1 = (batch + 1) * kForkBatch < n ? (batch + 1) * kForkBatch : n;
-  int parent[kForkBatch], child[kForkBatch], fork[kForkBatch];
+  const int of_batch = rows ? kRowBatch : kTileBatch, i1 = (batch + 1) * of_batch < n ? (batch + 1) * of_batch : n;
+  int parent[kRowBatch], child[kRowBatch], fork[kRowBatch];
+  static_assert(kTileBatch <= kRowBatch, "");
 #pragma unroll
-  for (int u = 0; u < kForkBatch; ++u) {
-    const int i = batch * kForkBatch + u < i1 ? P.order[batch * kForkBatch + u] : -1;
+  for (int u = 0; u < kRowBatch; ++u) {
+    const int i = batch * of_batch + u < i1 ? P.order[batch * of_batch + u] : -1;
     fork[u] = i;
     parent[u] = i >= 0 ? P.parent[i] : -1;
     child[u] = i >= 0 ? dst[i] : -1;
@@ -309,7 +310,7 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P
       sharers = 0;
     };
 #pragma unroll
-    for (int c = 0; c < kForkBatch; ++c) {
+    for (int c = 0; c < kRowBatch; ++c) {
       const int s = parent[c];
       if (s < 0) continue;
       const size_t from = (size_t)s * D.Hkv + g;
@@ -346,15 +347,15 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P
   __shared__ int lds[kCopyThreads / kWave];
   int held_of = -1, ctx = 0, nb = 0, before = 0;
 #pragma unroll
-  for (int c0 = 0; c0 < kForkBatch; ++c0) {
+  for (int c0 = 0; c0 < kTileBatch; ++c0) {
     const int s = parent[c0];
     if (s < 0 || s == held_of) continue;  // (its children are served with the first of them)
     held_of = s;
     ctx = ctx_len[s];
     nb = num_blocks(D, ctx);
-    if (g == 0 && part == 0 && threadIdx.x < kForkBatch) {
+    if (g == 0 && part == 0 && threadIdx.x < kTileBatch) {
 #pragma unroll
-      for (int c = 0; c < kForkBatch; ++c)
+      for (int c = 0; c < kTileBatch; ++c)
         if ((int)threadIdx.x == c && parent[c] == s) ctx_len[child[c]] = ctx;
     }
     const int32_t* row = table + ((size_t)s * D.Hkv + g) * D.max_blocks;
@@ -380,9 +381,9 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P
     for (int j = j0; j < j1; ++j) {
       const int e = row[j];
       if (!has_slot(e, P.n_slots)) continue;
-      int slot[kForkBatch];
+      int slot[kTileBatch];
 #pragma unroll
-      for (int c = 0; c < kForkBatch; ++c) {
+      for (int c = 0; c < kTileBatch; ++c) {
         slot[c] = -1;
         if (parent[c] != s) continue;
         const int rank = P.base[fork[c] * D.Hkv + g] + before;
@@ -394,7 +395,7 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(Dims D, Pages P
         TilePart T;
         T.load(k_pool, v_pool, (size_t)e * stride_bytes, at, tile_bytes);
 #pragma unroll
-        for (int c = 0; c < kForkBatch; ++c)
+        for (int c = 0; c < kTileBatch; ++c)
           if (slot[c] >= 0) T.store(k_pool, v_pool, (size_t)slot[c] * stride_bytes, at, tile_bytes);
       }
     }
@@ -578,17 +579,18 @@ int launch_fork(const Dims& D, int dtype, const Pages& P, int n, const int32_t* 
   const int es = dtype == SCOUT_BF16 ? 2 : 4;
   const int entry_bytes = D.digest_kind == 1 ? D.d * 4 : 2 * D.d * es, tile_bytes = D.S * D.d * es;
   const int row_blocks = kRowPieces * 16 / entry_bytes;  // 8 to 32
-  const long long pairs = (long long)(n + kForkBatch - 1) / kForkBatch * D.Hkv;
   const int row_parts = (D.max_blocks + row_blocks - 1) / row_blocks;
-  const long long row_wgs = row_parts * pairs;
-  // Table entries that a tile workgroup of a deep fork takes, one after the other: one where that gives no more workgroups than run at a
-  // time (2 heads of 65 blocks: 5.3 us for the launch, 8.6 with four), else four, which share the way to their first tile.
-  const int entries = pairs * D.max_blocks <= 2048 ? 1 : 4;
+  const long long row_wgs = (long long)(n + kRowBatch - 1) / kRowBatch * D.Hkv * row_parts;
+  // Table entries that a tile workgroup of a deep fork takes, one after the other.  Each counts the slots in front of its entries, all of a row
+  // at the end of it, which is little beside a tile up to 4096 blocks (2 children of 2 heads, 8 KiB tiles, 4096 blocks: one 51 us, four 60;
+  // 1024 blocks of 8 heads for 4 children: 64 and 71) and not beyond (16384 blocks: 366 and 343; of 2 KiB tiles: 140 and 82).
+  const int entries = D.max_blocks <= 4096 ? 1 : 4;
   const int parts = deep ? (D.max_blocks + entries - 1) / entries : 1;
-  if ((row_wgs + pairs * parts) * kCopyThreads >= 1ll << 32) return SCOUT_EUNSUPPORTED;  // threads of a launch
+  const long long tile_wgs = (long long)(n + kTileBatch - 1) / kTileBatch * D.Hkv * parts;
+  if ((row_wgs + tile_wgs) * kCopyThreads >= 1ll << 32) return SCOUT_EUNSUPPORTED;  // threads of a launch
   if (deep) hipLaunchKernelGGL(fork_count_kernel, dim3(n * D.Hkv), dim3(kCopyThreads), 0, st, D, P, src, ctx_len, table);
   hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, D, P, n, src, dst, deep, ctx_len, table, status);
-  hipLaunchKernelGGL(fork_copy_kernel, dim3((unsigned)(row_wgs + pairs * parts)), dim3(kCopyThreads), 0, st, D, P, n, dst, deep, ctx_len,
+  hipLaunchKernelGGL(fork_copy_kernel, dim3((unsigned)(row_wgs + tile_wgs)), dim3(kCopyThreads), 0, st, D, P, n, dst, deep, ctx_len,
                      static_cast<char*>(digest), entry_bytes, table, static_cast<char*>(k_pool), static_cast<char*>(v_pool), tile_bytes,
                      (long long)D.tile_stride * es, (int)row_wgs, row_blocks, row_parts, parts, entries);
   return launched();
