@@ -584,13 +584,17 @@ int launch_fork(const Dims& D, int dtype, const Pages& P, int n, const int32_t* 
   // Table entries that a tile workgroup of a deep fork takes, one after the other.  Each counts the slots in front of its entries, all of a row
   // at the end of it, which is little beside a tile up to 4096 blocks (2 children of 2 heads, 8 KiB tiles, 4096 blocks: one 51 us, four 60;
   // 1024 blocks of 8 heads for 4 children: 64 and 71) and not beyond (16384 blocks: 366 and 343; of 2 KiB tiles: 140 and 82).
-  const int entries = D.max_blocks <= 4096 ? 1 : 4;
-  const int parts = deep ? (D.max_blocks + entries - 1) / entries : 1;
-  const long long tile_wgs = (long long)(n + kTileBatch - 1) / kTileBatch * D.Hkv * parts;
-  if ((row_wgs + tile_wgs) * kCopyThreads >= 1ll << 32) return SCOUT_EUNSUPPORTED;  // threads of a launch
+  // More of them where a launch could not hold so many workgroups.
+  constexpr long long kMostWgs = (1ll << 32) / kCopyThreads - 1;
+  int entries = D.max_blocks <= 4096 ? 1 : 4;
+  auto parts_of = [&](int e) { return deep ? (D.max_blocks + e - 1) / e : 1; };
+  auto tile_wgs = [&](int e) { return (long long)(n + kTileBatch - 1) / kTileBatch * D.Hkv * parts_of(e); };
+  while (parts_of(entries) > 1 && row_wgs + tile_wgs(entries) > kMostWgs) entries *= 4;
+  const int parts = parts_of(entries);
+  if (row_wgs + tile_wgs(entries) > kMostWgs) return SCOUT_EUNSUPPORTED;
   if (deep) hipLaunchKernelGGL(fork_count_kernel, dim3(n * D.Hkv), dim3(kCopyThreads), 0, st, D, P, src, ctx_len, table);
   hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, D, P, n, src, dst, deep, ctx_len, table, status);
-  hipLaunchKernelGGL(fork_copy_kernel, dim3((unsigned)(row_wgs + tile_wgs)), dim3(kCopyThreads), 0, st, D, P, n, dst, deep, ctx_len,
+  hipLaunchKernelGGL(fork_copy_kernel, dim3((unsigned)(row_wgs + tile_wgs(entries))), dim3(kCopyThreads), 0, st, D, P, n, dst, deep, ctx_len,
                      static_cast<char*>(digest), entry_bytes, table, static_cast<char*>(k_pool), static_cast<char*>(v_pool), tile_bytes,
                      (long long)D.tile_stride * es, (int)row_wgs, row_blocks, row_parts, parts, entries);
   return launched();

@@ -414,3 +414,18 @@ def test_both_marshallers_pass_the_same():
         torch.cuda.synchronize()
         states.append([c.ctx, c.table, c.digest, c.k_pool, c.v_pool, c.pages[:60], *list(keep.values())])
     assert all(torch.equal(x, y) for x, y in zip(*states))
+
+
+@pytest.mark.parametrize("dtype,d,S", [(torch.bfloat16, 64, 16), (torch.float32, 64, 16)])
+def test_rows_of_many_blocks(dtype, d, S):
+    """Rows beyond 4096 blocks, with and without a slot, as long as a sequence can be and a few blocks shorter; freed slots that lie side by
+    side, and taken again."""
+    rng = np.random.default_rng(31)
+    mb = 4101
+    c = Cache(rng, 6, 1, S, d, dtype, mb, 5 * mb, [mb * S, (mb - 7) * S + 3, -1, -1, -1, -1], share=0.5, G=1)
+    assert (c.fork([0, 1, 0], [2, 3, 4], True) == 0).all()
+    c.free([2, 4])
+    c.fork([1, 3], [2, 4], True)
+    c.free([1])
+    c.compact()
+    c.fork([0], [5])
