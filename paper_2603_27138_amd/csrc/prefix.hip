@@ -435,8 +435,9 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(Pref
 //
 // Tiles by their rows (8 waves always; d = 128, 8 KV heads, 32k tokens):
 //   64   2 waves x 4 groups, 32 tokens   bound by memory: 227 MB of tiles in 46 us, 4.9 TB/s (read alone: 6.1); d = 64, 62 MB in 16 us
-//   128  4 waves x 2 groups, 64 tokens   by memory and the matrix instructions at once: 134 MB, 17 GFLOP in 29 us, 4.6 TB/s
-//   256  8 waves x 1 group, 128 tokens   by the matrix instructions and LDS: 68.7 GFLOP in 74 us, 930 TFLOP/s (a matrix product of 8192^3: 1206)
+//   128  4 waves x 2 groups, 64 tokens   by memory: 134 MB, 17 GFLOP in 36 to 39 us (3.6 TB/s; the loads alone, of 8 KiB tiles anywhere: 32)
+//   256  8 waves x 1 group, 128 tokens   by the matrix instructions and LDS: 68.7 GFLOP in 74 to 87 us, 790 to 930 TFLOP/s (a matrix product
+//                                        of 8192^3: 1206)
 // With 256 rows the two products alone take 33 us, the LDS reads that feed them 30, both 53 to 57: each wave reads all of a tile for its 32
 // rows.  64 rows a wave would read half, but their sums and logits do not fit in registers (they spill: 375 us).  Two waves of
 // a SIMD in opposite phases, another order of weights and products, raised priorities: no faster.
@@ -489,7 +490,7 @@ __global__ __launch_bounds__(WM* WN* kWave) void prefix_wide_kernel(PrefixPlan P
   constexpr int TILE = TOK * L::ROWB;                // bytes of K, and of V, of a tile
   constexpr int MINE = TILE / WM, NP = MINE / 1024;  // bytes and pieces of it that a wave brings
   constexpr int ROWS = TOK / WM;                     // token rows of it
-  constexpr int RING = 2;                            // (more of them, where there is room: no faster)
+  constexpr int RING = 2;                            // (three or four of 32 tokens for 128 rows: 38 to 39 us; of 64 for 256 rows: 92 to 96 against 87)
   typedef std::conditional_t<(UNITS > 4), uint64_t, uint32_t> Counts;  // tokens that count of each unit of a tile, a byte for each
   static_assert(UNITS <= 8 && ROWS <= 16 && MINE % 1024 == 0, "a wave's rows are of one unit, in whole pieces");
   static_assert(STEP <= 32, "steps are cut from 64 units");
