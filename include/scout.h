@@ -529,8 +529,8 @@ int scout_prefix_plan(const scout_problem* p, int32_t n_prefix, int32_t prefix_b
  * m is the reference that l and o are relative to: the largest logit, or up to 16 ln 2 below it
  * (m + ln l is the same).
  * Products, sums and softmax weights are binary32; with bf16 the weights enter the value
- * product as two bf16 terms (2^-15), or as one (2^-8) where o is not written and a
- * prefix has more than 64 rows (sequences times Hq / Hkv) on average.
+ * product as two bf16 terms for d = 128 (2^-15 of a weight), as three for d = 64 (2^-22),
+ * whoever is in the batch and whatever is written.
  */
 int shared_prefix_attn(const scout_problem* p, int32_t n_prefix, int32_t prefix_blocks,
                        const void* plan, size_t plan_bytes, const void* q, const void* k_pool,

@@ -204,11 +204,15 @@ __device__ __forceinline__ int query_row(const PrefixPlan& P, const PrefixWork& 
   return P.member[it.member0 + (int)m] * W.Hq + it.head * W.G + (int)(rr - m * W.G);
 }
 
-// bf16 terms of a softmax weight in the second product (bf16 only).  Two: 2^-15 of a weight at the most is lost.  One, rounded, where the
-// result leaves as bf16 and the matrix instructions bound the pass: half a step, 2^-8 of each weight at the most, about as much as the output's
-// own rounding (2-norm against binary64: 1.65e-3 for that alone, 2.2e-3 with one term, 1.7e-3 with two).  Two terms instead of one cost 1 to 6 %
-// up to 64 rows, 20 % at 128, 34 % at 256.  The sum l always has the weights as they are.
-constexpr int kOneTermFrom = 128;  // rows of a tile
+// bf16 terms of a softmax weight in the second product, for bf16.  All but the last are cut (7 explicit bits, what is left is below 2^-7), the last
+// one is rounded: two lose 2^-15 of a weight at the most, three 2^-22.  Three where the attention over a sequence's own tokens keeps its weights
+// in binary32 too, two where that one rounds them to a single term: what a batch shares is never held in fewer bits than what it does
+// not, whoever else is in the batch and whatever is written of the result.  The sum l always has the weights as they are.
+template <int DH>
+constexpr int kTerms = kWeights32<SCOUT_BF16, DH> ? 3 : 2;
+
+// A weight without its upper term.  Nothing left times an infinite value would be NaN: it is 2^-126.
+__device__ __forceinline__ float what_is_left(float w, uint32_t term) { return fmaxf(w - __uint_as_float(term), 0x1p-126f); }
 
 constexpr int kNarrowWaves = 8;
 
@@ -219,7 +223,7 @@ constexpr int kNarrowWaves = 8;
 template <int DT, int DH, int NQ>
 __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(PrefixPlan P, PrefixStamp stamp, PrefixWork W) {
   using L = Tile<DT, DH>;
-  constexpr int WAVES = kNarrowWaves, ROW = DH + 4, TERMS = 2;
+  constexpr int WAVES = kNarrowWaves, ROW = DH + 4, TERMS = kTerms<DH>;
   __shared__ float smem[WAVES * (16 * ROW + 32)];
   const PrefixItem it = P.item[blockIdx.x];  // in the trip that says whether it is one
   if (!made_for(P, stamp) || (int)blockIdx.x >= P.head[0]) return;
@@ -345,14 +349,10 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(Pref
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 hi[i] = __float_as_uint(p[i]) & 0xffff0000u;
-                p[i] -= __uint_as_float(hi[i]);
+                p[i] = what_is_left(p[i], hi[i]);
               }
               term[n] = __builtin_bit_cast(s16x4, (uint2){pack_halves(hi[0], hi[1], 1), pack_halves(hi[2], hi[3], 1)});
             } else {
-              if (TERMS > 1) {  // nothing left times an infinite value is not NaN
-#pragma unroll
-                for (int i = 0; i < 4; ++i) p[i] = fmaxf(p[i], 0x1p-126f);
-              }
               term[n] = __builtin_bit_cast(s16x4, (uint2){cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3])});
             }
           }
@@ -435,11 +435,11 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(Pref
 //
 // Tiles by their rows (8 waves always; d = 128, 8 KV heads, 32k tokens):
 //   64   2 waves x 4 groups, 32 tokens   bound by memory: 227 MB of tiles in 46 us, 4.9 TB/s (read alone: 6.1); d = 64, 62 MB in 16 us
-//   128  4 waves x 2 groups, 64 tokens   by memory: 134 MB, 17 GFLOP in 36 to 39 us (3.6 TB/s; the loads alone, of 8 KiB tiles anywhere: 32)
-//   256  8 waves x 1 group, 128 tokens   by the matrix instructions and LDS: 68.7 GFLOP in 74 to 87 us, 790 to 930 TFLOP/s (a matrix product
-//                                        of 8192^3: 1206)
-// With 256 rows the two products alone take 33 us, the LDS reads that feed them 30, both 53 to 57: each wave reads all of a tile for its 32
-// rows.  64 rows a wave would read half, but their sums and logits do not fit in registers (they spill: 375 us).  Two waves of
+//   128  4 waves x 2 groups, 64 tokens   by memory: 134 MB, 17 GFLOP in 37 to 42 us (3.2 to 3.6 TB/s; the loads alone: 32)
+//   256  8 waves x 1 group, 128 tokens   by the matrix instructions and LDS: 68.7 GFLOP in 98 to 121 us, 103 GFLOP with the second term of the
+//                                        weights, 0.85 to 1.05 PFLOP/s (a matrix product of 8192^3: 1.21)
+// With 256 rows and one term (74 to 87 us) the two products alone take 33 us, the LDS reads that feed them 30, both 53 to 57: each wave reads
+// all of a tile for its 32 rows.  64 rows a wave would read half, but their sums and logits do not fit in registers (they spill: 375 us).  Two waves of
 // a SIMD in opposite phases, another order of weights and products, raised priorities: no faster.
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
@@ -483,10 +483,10 @@ __device__ __forceinline__ void await() {
 // rows meets a larger logit, which is in most tiles.
 constexpr float kLag = 16.0f;
 
-template <int DH, int WM, int WN, int TOK, int TERMS>
+template <int DH, int WM, int WN, int TOK>
 __global__ __launch_bounds__(WM* WN* kWave) void prefix_wide_kernel(PrefixPlan P, PrefixStamp stamp, PrefixWork W) {
   using L = WideTile<DH>;
-  constexpr int NH = TOK / 32, UNITS = TOK / 16, STEP = UNITS * WN;
+  constexpr int NH = TOK / 32, UNITS = TOK / 16, STEP = UNITS * WN, TERMS = kTerms<DH>;
   constexpr int TILE = TOK * L::ROWB;                // bytes of K, and of V, of a tile
   constexpr int MINE = TILE / WM, NP = MINE / 1024;  // bytes and pieces of it that a wave brings
   constexpr int ROWS = TOK / WM;                     // token rows of it
@@ -648,10 +648,8 @@ __global__ __launch_bounds__(WM* WN* kWave) void prefix_wide_kernel(PrefixPlan P
           if (n + 1 < TERMS) {  // cut, not rounded: what is left is not negative
             const uint32_t a = __float_as_uint(w[e]), b = __float_as_uint(w[e + 1]);
             packed[e / 2] = pack_halves(a, b, 1);
-            w[e] -= __uint_as_float(a & 0xffff0000u);
-            w[e + 1] -= __uint_as_float(b & 0xffff0000u);
-          } else if (TERMS > 1) {  // nothing left times an infinite value is not NaN
-            packed[e / 2] = cvt_pk_bf16(fmaxf(w[e], 0x1p-126f), fmaxf(w[e + 1], 0x1p-126f));
+            w[e] = what_is_left(w[e], a & 0xffff0000u);
+            w[e + 1] = what_is_left(w[e + 1], b & 0xffff0000u);
           } else {
             packed[e / 2] = cvt_pk_bf16(w[e], w[e + 1]);
           }
@@ -921,12 +919,6 @@ int launch_prefix_plan(const Dims& D, int dtype, int n_prefix, int prefix_blocks
   return hipGetLastError() == hipSuccess ? SCOUT_OK : SCOUT_EHIP;
 }
 
-template <int DH, int TERMS>
-static void launch_many_rows(const PrefixShape& s, int grid, const PrefixPlan& P, const PrefixStamp& stamp, const PrefixWork& W, hipStream_t st) {
-  if (s.tile_rows == 128) hipLaunchKernelGGL((prefix_wide_kernel<DH, 4, 2, 64, TERMS>), dim3(grid), dim3(512), 0, st, P, stamp, W);
-  else hipLaunchKernelGGL((prefix_wide_kernel<DH, 8, 1, 128, TERMS>), dim3(grid), dim3(512), 0, st, P, stamp, W);
-}
-
 template <int DT, int DH>
 static void launch_all(const Dims& D, const PrefixShape& s, int items, const PrefixPlan& P, const PrefixStamp& stamp, const PrefixWork& W,
                        const PrefixOut& E, hipStream_t st) {
@@ -936,10 +928,9 @@ static void launch_all(const Dims& D, const PrefixShape& s, int items, const Pre
   } else if (s.tile_rows == 32) {
     hipLaunchKernelGGL((prefix_narrow_kernel<DT, DH, 2>), g, dim3(512), 0, st, P, stamp, W);
   } else if constexpr (DT == SCOUT_BF16) {
-    static_assert(kOneTermFrom == 128, "below, two");
-    if (s.tile_rows == 64) hipLaunchKernelGGL((prefix_wide_kernel<DH, 2, 4, 32, 2>), g, dim3(512), 0, st, P, stamp, W);
-    else if (E.o != nullptr) launch_many_rows<DH, 2>(s, items, P, stamp, W, st);
-    else launch_many_rows<DH, 1>(s, items, P, stamp, W, st);
+    if (s.tile_rows == 64) hipLaunchKernelGGL((prefix_wide_kernel<DH, 2, 4, 32>), g, dim3(512), 0, st, P, stamp, W);
+    else if (s.tile_rows == 128) hipLaunchKernelGGL((prefix_wide_kernel<DH, 4, 2, 64>), g, dim3(512), 0, st, P, stamp, W);
+    else hipLaunchKernelGGL((prefix_wide_kernel<DH, 8, 1, 128>), g, dim3(512), 0, st, P, stamp, W);
   }
   hipLaunchKernelGGL((prefix_combine_kernel<DT, DH>), dim3((D.B * D.Hq + 3) / 4), dim3(256), 0, st, P, stamp, W, E);
 }
