@@ -211,8 +211,11 @@ __device__ __forceinline__ int query_row(const PrefixPlan& P, const PrefixWork& 
 template <int DH>
 constexpr int kTerms = kWeights32<SCOUT_BF16, DH> ? 3 : 2;
 
-// A weight without its upper term.  Nothing left times an infinite value would be NaN: it is 2^-126.
-__device__ __forceinline__ float what_is_left(float w, uint32_t term) { return fmaxf(w - __uint_as_float(term), 0x1p-126f); }
+// A weight without its upper term.  Nothing left times an infinite value would be NaN, so of a weight there is always 2^-126 left (the least
+// that one has; the bounds above are those of weights from 2^-104 on).  Of no weight nothing is: 2^-126 of the largest value would be 4.
+__device__ __forceinline__ float what_is_left(float w, uint32_t term) {
+  return __builtin_amdgcn_fmed3f(w - __uint_as_float(term), 0x1p-126f, w);
+}
 
 constexpr int kNarrowWaves = 8;
 

@@ -85,3 +85,23 @@ def test_fp32_keeps_its_weights_whole():
     b = Batch(5, F32, 64, 16, 8, 1, [3, 700], _of(2, 30))
     b.run(partial=True).check()
     assert math.isfinite(float(b.o.abs().max()))
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("n", COUNTS)
+def test_large_values_without_weight(d, n):
+    """The largest finite value of tokens whose logits are 400 below the others': their weights are zero in binary32 and below 2^-577 in
+    truth, and nothing of the value may be seen."""
+    b = Batch(n, BF16, d, 32, 8, 2, [40, 300], _of(2, n), scale=0.125)
+    b.q = torch.zeros(b.q.shape, dtype=BF16)
+    b.q[..., 5] = 4.0
+    b.k = torch.where(b.k.isnan(), b.k, torch.zeros_like(b.k))
+    for p, tokens in ((0, (7, 33)), (1, (0, 130, 299))):
+        for g in range(b.Hkv):
+            for t in tokens:
+                s = int(b.table[p, g, t // 32])
+                b.k[s, t % 32, 5] = -800.0
+                b.v[s, t % 32] = torch.finfo(BF16).max
+    b.k_dev, b.v_dev = b.k.cuda(), b.v.cuda()
+    _check(b.run(partial=True))
+    _check(b.run())
