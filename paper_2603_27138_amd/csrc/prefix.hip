@@ -464,16 +464,16 @@ __device__ __forceinline__ void load_to_lds(const void* base, int bytes, const i
   static_assert(N == 1 || N == 2 || N == 4, "pieces");
   // a scalar write of m0 needs a wait state in front of the load that uses it
   if constexpr (N == 1)
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %0, 0 offen lds" ::"s"(rsrc), "s"(to), "v"(at[0]) : "memory");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %0, 0 offen lds" ::"s"(rsrc), "s"(to), "v"(at[0]) : "memory", "m0");
   else if constexpr (N == 2)
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %0, 0 offen lds\n\t"
                  "buffer_load_dwordx4 %3, %0, 0 offen offset:1024 lds" ::"s"(rsrc), "s"(to), "v"(at[0]), "v"(at[1])
-                 : "memory");
+                 : "memory", "m0");
   else
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %0, 0 offen lds\n\t"
                  "buffer_load_dwordx4 %3, %0, 0 offen offset:1024 lds\n\tbuffer_load_dwordx4 %4, %0, 0 offen offset:2048 lds\n\t"
                  "buffer_load_dwordx4 %5, %0, 0 offen offset:%6 lds" ::"s"(rsrc), "s"(to), "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(3 * 1024)
-                 : "memory");
+                 : "memory", "m0");
 }
 // All but the last N of the wave's loads from memory have arrived, and what it has read of LDS.
 template <int N>
