@@ -482,6 +482,13 @@ __device__ __forceinline__ void await() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
 }
 
+// Between what lanes of a wave store in LDS and what other lanes of it read there, and the other way round: LDS serves a wave's accesses in order, the
+// compiler has to keep that order (no instruction).
+__device__ __forceinline__ void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // A row's sums are kept relative to a number that follows its maximum only when that has moved by more than 2^kLag: weights are below 2^kLag then,
 // which binary32 sums and bf16 terms hold as well as weights below one, and the sums need not be rescaled whenever one of a wave's
 // rows meets a larger logit, which is in most tiles.
@@ -542,7 +549,9 @@ __global__ __launch_bounds__(WM* WN* kWave) void prefix_wide_kernel(PrefixPlan P
     }
     u_pos = 0;
     u_n = n;
+    wave_exchange();
     const int2 mine = q[lane];
+    wave_exchange();
     u_slot = mine.x;
     u_what = lane < n ? mine.y : 0;
     u_full = __ballot((u_what & 255) == kUnitTokens);
@@ -733,6 +742,7 @@ __global__ __launch_bounds__(WM* WN* kWave) void prefix_wide_kernel(PrefixPlan P
         const int r = c / L::CH;
         if (r % 16 >= (int)(tokens >> (8 * (r / 16)) & 255)) *reinterpret_cast<u32x4*>(v + c * 16) = (u32x4){0, 0, 0, 0};
       }
+      wave_exchange();
       follow(largest());
       values(v);
     }
