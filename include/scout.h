@@ -298,6 +298,8 @@ int merge_partials(const scout_problem* p, const float* o_a, const float* m_a, c
  * both ascending by block index; the i-th recalled block takes the slot of the
  * i-th evicted block and block_table is updated in place.  The caller copies
  * the recalled tiles into the returned slots before the next step's attention.
+ * A slot that other sequences name too (a shallow fork_sequences) must not be evicted
+ * here: they would read the recalled block's tiles as theirs.
  *   block_table  i32 [B][Hkv][max_blocks]   in/out
  *   recall_blk, recall_slot, evict_blk  i32 [B][Hkv][k]   out, padded with -1
  *   n_recall     i32 [B][Hkv]   out
@@ -407,11 +409,20 @@ int scout_layer_step(const scout_problem* p, const void* q, const void* digest,
  *     as it is, and it has no blocks.
  *   - A shared tile is not written to: only full blocks are shared by a fork.
  *     periodic_recall gives an evicted block's slot to another block of its pair, so
- *     it is for pairs that hold their slots alone (fork with deep = 1).
+ *     it is for pairs that hold their slots alone (fork with deep = 1); it knows nothing
+ *     of the counts and refuses nothing.
  *   - Calls on the same state must be ordered (one stream, or events).
  *
  * shared_prefix_attn reads nothing of the pages' state: prefix_table is a table of
  * slots like any other.
+ *
+ * Either a sequence's row names the shared blocks, or shared_prefix_attn attends to
+ * them, not both: scout_layer_step and what it is made of select among all blocks of a
+ * row, and a fork's row names its parent's.  Joined with shared_prefix_attn over the same
+ * blocks they would count twice.  In a batch that uses shared_prefix_attn the prefix has
+ * a row of its own (a prompt's, which prefix_table may be a part of), and the sequences'
+ * rows begin behind it, with ctx_len the number of their own tokens; they can be forked
+ * from one another as any others.
  */
 
 /* Bytes of the pages' state of a pool of n_slots slots (at most 2^29). */
