@@ -402,9 +402,10 @@ int scout_layer_step(const scout_problem* p, const void* q, const void* digest,
  * bytes in DEVICE memory, 16-byte aligned, whose first n_slots words are these counts
  * (int32, 0: the slot is free) and whose rest is the library's.  scout_pages_init
  * makes it from the block tables; from then on the calls below keep it current, and a
- * table entry that they do not know of (one that the caller writes by itself) is a
- * slot that they may give away.  Slots are taken lowest first, in the order of the
- * takers, so that the same state gives the same slots.
+ * table entry that they do not know of (one that the caller writes by itself, of a slot
+ * that reserve_blocks did not give it) is a slot that they may give away.  Slots are
+ * taken lowest first, in the order of the takers, so that the same state gives the same
+ * slots.
  *   - A row of the batch without a sequence has ctx_len -1: append_token leaves it
  *     as it is, and it has no blocks.
  *   - A shared tile is not written to: only full blocks are shared by a fork.
@@ -448,6 +449,9 @@ int scout_pages_init(const scout_problem* p, const int32_t* ctx_len, int32_t* bl
  * A reserved slot counts as held from here on; the append that follows puts it into
  * the table.  Until then no row names it: reserve once for an append, and free or fork
  * onto a sequence only behind it, or the slot stays held.
+ * A prompt that is admitted takes the slots of its n blocks in one call, with a problem
+ * of B = n and n zeros as its ctx_len: new_slot [n][Hkv] is then the caller's to put into
+ * the prompt's row ([Hkv][n], the rest of the row -1) before it sets the row's ctx_len.
  *   new_slot  i32 [B][Hkv]  out: append_token's argument
  *   n_short   i32 [1]       out: takers for whom no slot was left
  */
