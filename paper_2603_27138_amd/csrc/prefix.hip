@@ -461,12 +461,10 @@ template <int N>
 __device__ __forceinline__ void load_to_lds(const void* base, int bytes, const int (&at)[N], uint32_t to) {
   const uint64_t b = reinterpret_cast<uint64_t>(base);
   const i32x4 rsrc = {(int)(uint32_t)b, (int)(uint32_t)(b >> 32) & 0xffff, bytes, 0x00020000};
-  static_assert(N == 1 || N == 2 || N == 4, "pieces");
+  static_assert(N == 2 || N == 4, "pieces");
   // One wait state between the write of m0 and the load that uses it; five between a vector instruction that wrote a scalar operand, which the
   // compiler knows of and the loads here it does not, and the load that reads it.
-  if constexpr (N == 1)
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tbuffer_load_dwordx4 %2, %0, 0 offen lds" ::"s"(rsrc), "s"(to), "v"(at[0]) : "memory", "m0");
-  else if constexpr (N == 2)
+  if constexpr (N == 2)
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tbuffer_load_dwordx4 %2, %0, 0 offen lds\n\t"
                  "buffer_load_dwordx4 %3, %0, 0 offen offset:1024 lds" ::"s"(rsrc), "s"(to), "v"(at[0]), "v"(at[1])
                  : "memory", "m0");
