@@ -4,7 +4,8 @@
 //   x_t = scale q_bh . k_t,  m = max x_t,  l = sum exp(x_t - m),  o = sum exp(x_t - m) v_t / l
 // over the prefix's tokens that have a slot.  Attended to sequence by sequence the prefix's tiles are read once per sequence; here
 // the heads of all its sequences are rows of one product with every tile, which is read once per tile of rows: n sequences read
-// 1/n of the bytes, and beyond some 190 rows a KV head (1.15 PFLOP/s over 6.2 TB/s) it is the matrix instructions that bound it.
+// 1/n of the bytes, and beyond some 130 rows a KV head (6 flop a row for 4 bytes, 1.2 PFLOP/s over 6.2 TB/s) it is the matrix instructions
+// that bound it.
 //
 // prefix_plan_kernel deals the work once for a batch (the lengths of prefixes and who has them do not change with the layer);
 // prefix_attn_kernel leaves a partial per row and split; prefix_combine_kernel folds them, with the sequence's own partial.
@@ -223,6 +224,7 @@ constexpr int kNarrowWaves = 8;
 // into MFMA operand registers, and NQ column tiles of 16 rows are multiplied with them there (layout: see attn_unit.h).  The waves fold through LDS.
 // Bound by memory, and where there is little of it by a launch's way in and out: 4 sequences of 4 heads over 8192 shared tokens (8 KV heads,
 // 33.5 MB at bf16, d = 128) 8 us, of which 2.3 are the launch and 4 the way to the first unit and from the last; 2 of them over 65536 tokens 42 us (6.4 TB/s).
+// With the fold's launch: 16 rows 9 us and each byte at 6.1 TB/s, 32 rows 13 and 5.9, fp32 11 and 6.0 (16 rows), 15 and 5.5 (32).
 template <int DT, int DH, int NQ>
 __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(PrefixPlan P, PrefixStamp stamp, PrefixWork W) {
   using L = Tile<DT, DH>;
@@ -437,13 +439,16 @@ __global__ __launch_bounds__(kNarrowWaves* kWave) void prefix_narrow_kernel(Pref
 // Units of 16 tokens without a slot are left out: every tile but an item's last one is full.
 //
 // Tiles by their rows (8 waves always; d = 128, 8 KV heads, 32k tokens):
-//   64   2 waves x 4 groups, 32 tokens   bound by memory: 227 MB of tiles in 46 us, 4.9 TB/s (read alone: 6.1); d = 64, 62 MB in 16 us
-//   128  4 waves x 2 groups, 64 tokens   by memory: 134 MB, 17 GFLOP in 37 to 42 us (3.2 to 3.6 TB/s; the loads alone: 32)
-//   256  8 waves x 1 group, 128 tokens   by the matrix instructions and LDS: 68.7 GFLOP in 98 to 121 us, 103 GFLOP with the second term of the
-//                                        weights, 0.85 to 1.05 PFLOP/s (a matrix product of 8192^3: 1.21)
-// With 256 rows and one term (74 to 87 us) the two products alone take 33 us, the LDS reads that feed them 30, both 53 to 57: each wave reads
-// all of a tile for its 32 rows.  64 rows a wave would read half, but their sums and logits do not fit in registers (they spill: 375 us).  Two waves of
-// a SIMD in opposite phases, another order of weights and products, raised priorities: no faster.
+//   64   2 waves x 4 groups, 32 tokens   bound by memory: 227 MB of tiles in 46 us, 4.9 TB/s (read alone: 6.1); d = 64, 62 MB in 20 us
+//   128  4 waves x 2 groups, 64 tokens   by memory, and the way in and out: 134 MB, 26 GFLOP in 37 to 42 us
+//   256  8 waves x 1 group, 128 tokens   by the matrix instructions and LDS: 103 GFLOP in 98 to 121 us, 0.85 to 1.05 PFLOP/s (a matrix product
+//                                        of 8192^3: 1.21)
+// With the fold's launch: 64 rows 15 us and each byte at 5.8 TB/s, 128 rows 18 and 4.6, d = 64 and 64 rows 10 and 4.2 (two tiles of a group are 16 KB there,
+// half of what is in flight at d = 128).
+// With 256 rows attention and fold take 113 us, without the matrix instructions 60, without the LDS reads that feed them 87, without these and
+// the exponentials 83: each wave reads all of a tile for its 32 rows.  64 rows a wave would read half; with the next tile's logits held as well, to have
+// both products at hand, they spill (375 us).  Two waves of a SIMD in opposite phases, another order of weights and products, raised
+// priorities: no faster.
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 
@@ -891,7 +896,15 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(PrefixPlan P, Prefi
 
 // ---------------------------------------------------------------- launches
 
-// How the work of a batch is dealt: by the rows that a prefix has on average (the rows of a prefix with more are several tiles).
+// How the work of a batch is dealt: by the rows that a prefix has on average (the rows of a prefix with more are several tiles), the least tile that
+// holds them.  Attention and fold, 8 KV heads of 128 channels, one prefix, us with the smaller | the larger tile:
+//   16 | 32    24 rows: 32k tokens 36 | 35, 128k 108 | 102; fp32, 32 rows: 8k tokens 23 | 26, 64k 119 | 112
+//   32 | 64    48 rows: 32k 39.9 | 39.2; 64 rows: 128k 114 | 105
+//   64 | 128   96 rows: 32k 46.9 | 46.9; 128 rows: 128k 145 | 129
+//   128 | 256  192 rows: 32k 63.7 | 65.4, 256 rows: 69.7 | 68.2, 128k 220 | 199
+// Over a few thousand tokens smaller tiles are faster, having more workgroups (64 rows, 4096 tokens: 13.5 with 16, 17.4 with 64).
+// granule: a step of every kernel is 128 tokens; 64, 128 and 256 differ by 1 %, and short prefixes have more splits with 64.
+// head_cost: 48 sequences over five prefixes of 3000 to 24000 tokens 83 us with 0 and 128, 78 with 256, 512 and 1024; others within 2 %.
 static PrefixShape prefix_shape(const Dims& D, int dtype, int n_prefix) {
   const long long rows = ((long long)D.B * D.G + n_prefix - 1) / (n_prefix > 0 ? n_prefix : 1);
   PrefixShape s;
