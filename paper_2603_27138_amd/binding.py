@@ -216,6 +216,12 @@ def _bytes(t: torch.Tensor) -> int:
     return t.numel() * t.element_size()
 
 
+def _count(n) -> int:
+    """A number that the library takes in 32 bits: beyond them -1, which it refuses."""
+    n = int(n)
+    return n if -2 ** 31 <= n < 2 ** 31 else -1
+
+
 def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
@@ -474,7 +480,7 @@ def compact_pool(p: Problem, block_table, k_pool, v_pool, n_slots, pages, slot_m
 
 def prefix_plan_bytes(p: Problem, n_prefix: int) -> int:
     n = ctypes.c_size_t(0)
-    _check("scout_prefix_plan_bytes", lib().scout_prefix_plan_bytes(ctypes.byref(p), int(n_prefix), ctypes.byref(n)))
+    _check("scout_prefix_plan_bytes", lib().scout_prefix_plan_bytes(ctypes.byref(p), _count(n_prefix), ctypes.byref(n)))
     return n.value
 
 
@@ -486,7 +492,7 @@ def prefix_plan(p: Problem, n_prefix, prefix_blocks, prefix_of, prefix_len, plan
     """Once for a batch: who has which prefix, and how the attention over them is dealt to workgroups."""
     if _recording is None:
         return _done("scout_prefix_plan", (_calls or _load_calls()).prefix_plan(p, n_prefix, prefix_blocks, prefix_of, prefix_len, plan))
-    _call("scout_prefix_plan", lib().scout_prefix_plan, ctypes.byref(p), int(n_prefix), int(prefix_blocks), _ptr_here(prefix_of),
+    _call("scout_prefix_plan", lib().scout_prefix_plan, ctypes.byref(p), _count(n_prefix), _count(prefix_blocks), _ptr_here(prefix_of),
           _ptr_here(prefix_len), _ptr_here(plan), _bytes(plan), _stream())
 
 
@@ -497,7 +503,7 @@ def shared_prefix_attn(p: Problem, n_prefix, prefix_blocks, plan, q, k_pool, v_p
     if _recording is None:
         return _done("shared_prefix_attn", (_calls or _load_calls()).shared_prefix_attn(
             p, n_prefix, prefix_blocks, plan, q, k_pool, v_pool, n_slots, prefix_table, o_b, m_b, l_b, o, m, l, out, lse, ws))
-    _call("shared_prefix_attn", lib().shared_prefix_attn, ctypes.byref(p), int(n_prefix), int(prefix_blocks), _ptr_here(plan),
+    _call("shared_prefix_attn", lib().shared_prefix_attn, ctypes.byref(p), _count(n_prefix), _count(prefix_blocks), _ptr_here(plan),
           _bytes(plan), _ptr_here(q), _ptr_here(k_pool), _ptr_here(v_pool), int(n_slots), _ptr_here(prefix_table), _ptr_here(o_b),
           _ptr_here(m_b), _ptr_here(l_b), _ptr_here(o), _ptr_here(m), _ptr_here(l), _ptr_here(out), _ptr_here(lse), _ptr_here(ws),
           _bytes(ws), _stream())

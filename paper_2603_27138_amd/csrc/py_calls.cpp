@@ -171,6 +171,16 @@ struct Args {
     if (v == -1 && PyErr_Occurred()) ok = false;
     return v;
   }
+  // a number that the library takes in 32 bits: beyond them -1, which it refuses
+  int32_t count() {
+    if (!ok) return 0;
+    PyObject* const as_int = PyNumber_Long(next());
+    int beyond = 0;
+    const long long v = as_int ? PyLong_AsLongLongAndOverflow(as_int, &beyond) : -1;
+    Py_XDECREF(as_int);
+    if (v == -1 && PyErr_Occurred()) ok = false;
+    return beyond || v != (int32_t)v ? -1 : (int32_t)v;
+  }
 };
 
 void* current_stream() {
@@ -462,18 +472,18 @@ PyObject* py_prefix_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Args A("scout_prefix_plan", a, n, 6);
   const auto* p = A.prob();
   A.here();
-  const int64_t prefixes = A.integer(), blocks = A.integer();
+  const i32 prefixes = A.count(), blocks = A.count();
   i32 *of = A.dev<i32>(), *len = A.dev<i32>();
   size_t nplan;
   void* plan = A.buffer(&nplan);
-  SCOUT_RETURN(T.scout_prefix_plan(p, (i32)prefixes, (i32)blocks, of, len, plan, nplan, st));
+  SCOUT_RETURN(T.scout_prefix_plan(p, prefixes, blocks, of, len, plan, nplan, st));
 }
 
 PyObject* py_shared_prefix_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Args A("shared_prefix_attn", a, n, 18);
   const auto* p = A.prob();
   A.here();
-  const int64_t prefixes = A.integer(), blocks = A.integer();
+  const i32 prefixes = A.count(), blocks = A.count();
   size_t nplan;
   void* plan = A.buffer(&nplan);
   void *q = A.dev(), *kp = A.dev(), *vp = A.dev();
@@ -485,7 +495,7 @@ PyObject* py_shared_prefix_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   float* lse = A.dev<float>();
   size_t nws;
   void* ws = A.buffer(&nws);
-  SCOUT_RETURN(T.shared_prefix_attn(p, (i32)prefixes, (i32)blocks, plan, nplan, q, kp, vp, slots, table, ob, mb, lb, o, m, l, out,
+  SCOUT_RETURN(T.shared_prefix_attn(p, prefixes, blocks, plan, nplan, q, kp, vp, slots, table, ob, mb, lb, o, m, l, out,
                                     lse, ws, nws, st));
 }
 
