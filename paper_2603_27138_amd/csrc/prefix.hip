@@ -504,7 +504,7 @@ __global__ __launch_bounds__(WM* WN* kWave) void prefix_wide_kernel(PrefixPlan P
   constexpr int TILE = TOK * L::ROWB;                // bytes of K, and of V, of a tile
   constexpr int MINE = TILE / WM, NP = MINE / 1024;  // bytes and pieces of it that a wave brings
   constexpr int ROWS = TOK / WM;                     // token rows of it
-  constexpr int RING = 2;                            // (three or four of 32 tokens for 128 rows: 38 to 39 us; of 64 for 256 rows: 92 to 96 against 87)
+  constexpr int RING = 2;                            // (d = 128, one term of a weight: three or four of 32 tokens for 128 rows 38 to 39 us against 36 to 39; of 64 for 256 rows 92 to 96 against 87)
   typedef std::conditional_t<(UNITS > 4), uint64_t, uint32_t> Counts;  // tokens that count of each unit of a tile, a byte for each
   static_assert(UNITS <= 8 && ROWS <= 16 && MINE % 1024 == 0, "a wave's rows are of one unit, in whole pieces");
   static_assert(STEP <= 32, "steps are cut from 64 units");
